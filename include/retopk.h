@@ -253,6 +253,144 @@ retopk_status retopk_profile_read(retopk_handle h, int32_t n_kernels, uint64_t *
                                   double *total_ms);
 const char *retopk_kernel_name(int32_t kernel_id);   /* NULL past the last id */
 
+/* ---------------------------------------------------------------------------
+ * Rotary positions and the paged cache: what surrounds the attention calls.
+ *
+ * These calls need no handle.  They take the current HIP device, to which the
+ * stream and every pointer must belong, allocate nothing, never synchronise and
+ * can be captured in a HIP graph; two calls may overlap as long as neither writes
+ * what the other touches (a workspace included).
+ *
+ * A paged cache holds the rows of n_seqs sequences in pages of page_size positions:
+ * position p of sequence s is row p % page_size of page table[s * table_width +
+ * p / page_size].  Pages are [n_pages, Hkv, page_size, row], K and V apart, so that a
+ * cache of f32 or bf16 pages with page_size = max_len and table[b] = b is the layout
+ * [B, Hkv, max_len, d] that retopk_decode_step and its baselines take: paged_append
+ * writes it, they read it.
+ *
+ * 4-bit rows (RETOPK_PAGES_Q4) hold the d codes in d / 2 bytes and, in k_par and v_par
+ * [n_pages, Hkv, page_size, d / 64], one word for every 64 elements: its low half is the
+ * bf16 scale, its high half the bf16 middle of the group.  An element is
+ * mid + scale * c with c one of -7.5, -6.5 .. 7.5, held as a sign bit s and the three
+ * bits m of |c| - 1/2.  The bytes b0, b1 of the elements 4 i .. 4 i + 3 hold, from the
+ * top bit, s2 m0 s3 m1 and s0 m2 s1 m3.  paged_append chooses, in 64 bits from the
+ * group's float32 values x: mid = bf16((max + min) / 2), scale = bf16(max(max - mid,
+ * mid - min) / 7.5), c = clamp(floor((x - mid) / scale), -8, 7) + 1/2 (mid itself where
+ * scale is 0).  A row takes d / 2 + d / 16 bytes: 72 for d = 128, where bf16 takes 256.
+ * ------------------------------------------------------------------------- */
+
+typedef enum { RETOPK_PAGES_F32 = 0, RETOPK_PAGES_BF16 = 1, RETOPK_PAGES_Q4 = 2 } retopk_page_format;
+
+typedef struct {
+    int32_t format;        /* retopk_page_format; f32 and bf16 pages go with q, k and v   */
+                           /* of that type, 4-bit pages with either                       */
+    int32_t n_kv_heads;    /* Hkv >= 1                                                    */
+    int32_t head_dim;      /* d in {64, 128}                                              */
+    int32_t page_size;     /* positions of a page, >= 1; 4-bit: a multiple of 16          */
+    int32_t n_pages;       /* >= 1; n_pages * Hkv * page_size < 2^31                      */
+    int32_t n_seqs;        /* >= 1                                                        */
+    int32_t table_width;   /* >= 1; page_size * table_width < 2^31                        */
+    void *k, *v;           /* device, 16-byte aligned                                     */
+    uint32_t *k_par, *v_par;  /* 4-bit: device, 16-byte aligned; else ignored             */
+    const int32_t *table;  /* device [n_seqs, table_width]; an id outside [0, n_pages)    */
+                           /* is no page: nothing is written to it or read from it        */
+} retopk_pages;
+
+/* Rows of d elements of a tensor [tokens, heads, d] whose last dimension is dense: element
+ * (t, h, e) at p + t * token_stride + h * head_stride + e, strides in elements.  p must be
+ * 16-byte aligned and the strides non-negative multiples of 16 bytes. */
+typedef struct { void *p; int64_t token_stride, head_stride; } retopk_rows;
+
+/* Rotation of the first rot_dim elements of a head by angles pos * freq[i], pair i being
+ * elements (i, i + rot_dim / 2), or (2 i, 2 i + 1) when interleaved; factor scales the
+ * rotated elements.  Filled by retopk_rope_init or by hand; host memory. */
+typedef struct {
+    int32_t rot_dim;       /* even, 2 .. head_dim                                         */
+    int32_t interleaved;   /* 0 or 1                                                      */
+    double factor;         /* finite                                                      */
+    double freq[64];       /* radians a position, finite                                  */
+} retopk_rope;
+
+/* Frequencies for contexts past the trained one (inv = theta^(-2 i / rot_dim)):
+ *   LINEAR  inv / factor: positions interpolated
+ *   NTK     theta scaled by factor^(rot_dim / (rot_dim - 2)): the lowest frequency divided
+ *           by factor, the highest kept
+ *   BANDS   by the turns n a pair makes over original_len positions: inv from `high` turns
+ *           on, inv / factor up to `low`, between them the mix linear in n
+ *   RAMP    the same mix linear in the pair's index, from that of `high` turns (rounded
+ *           down) to that of `low` (rounded up), and rotated elements scaled by
+ *           0.1 ln(factor) + 1                                                            */
+typedef enum { RETOPK_ROPE_PLAIN = 0, RETOPK_ROPE_LINEAR = 1, RETOPK_ROPE_NTK = 2,
+               RETOPK_ROPE_BANDS = 3, RETOPK_ROPE_RAMP = 4 } retopk_rope_kind;
+typedef struct {
+    int32_t kind;          /* retopk_rope_kind                                            */
+    double factor;         /* >= 1                                                        */
+    double original_len;   /* BANDS and RAMP: the trained context, > 0                    */
+    double low, high;      /* BANDS and RAMP: turns, 0 < low < high                       */
+} retopk_rope_scaling;
+
+/* Fill *r (host only).  theta > 1; scaling NULL: plain.  RETOPK_ERR_ARG for anything
+ * outside the ranges above (NTK needs rot_dim > 2), and *r is then left alone. */
+retopk_status retopk_rope_init(retopk_rope *r, int32_t rot_dim, int32_t interleaved,
+                               double theta, const retopk_rope_scaling *scaling);
+
+/* out = x rotated to positions pos[t] (any int32), pair (a, b) by angle phi to
+ * factor * (a cos phi - b sin phi, a sin phi + b cos phi); with inverse, to
+ * factor * (a cos phi + b sin phi, b cos phi - a sin phi), which is the gradient of x
+ * for the gradient x of out.  Computed in float64, rounded to float32 and then to dtype
+ * (retopk_dtype); elements past rot_dim are copied.  out may be x itself (same pointer and
+ * strides), and must not overlap it otherwise. */
+retopk_status rotary_embed(const retopk_rope *r, int32_t dtype, int32_t head_dim,
+                           int32_t n_heads, int64_t n_tokens, const int32_t *pos,
+                           retopk_rows x, retopk_rows out, int32_t inverse, void *stream);
+
+/* Append: row t of k and v [n_tokens, Hkv, d] goes to position pos[t] of sequence seq[t],
+ * k rotated to that position on the way (r NULL: as it is), and q [n_tokens, n_q_heads, d],
+ * rotated likewise, to q_out (n_q_heads = 0: no queries; else r must be given; q_out may be
+ * q as in rotary_embed).  A token whose seq is outside [0, n_seqs) is padding: neither the
+ * cache nor its row of q_out is written; one whose position has no page gets its q_out row
+ * only.  Every other row of the cache is left as it was.  No position of a sequence may
+ * appear twice in a call (which of the two rows the cache then holds, or what mix of
+ * them, is unspecified).  k and v must be finite for 4-bit pages: a non-finite element
+ * leaves its group of 64 unspecified. */
+retopk_status paged_append(const retopk_pages *c, const retopk_rope *r, int32_t dtype,
+                           int64_t n_tokens, const int32_t *seq, const int32_t *pos,
+                           retopk_rows k, retopk_rows v, int32_t n_q_heads, retopk_rows q,
+                           retopk_rows q_out, void *stream);
+
+/* The reverse: position pos[t] of sequence seq[t] read into row t of k and v
+ * [n_tokens, Hkv, d] of type dtype (4-bit rows as the values they stand for, in float32
+ * and then rounded to dtype); k.p or v.p may be NULL.  Rows without a page are left as they
+ * were.  With token_stride d and head_stride max_len * d, the rows of one sequence land
+ * in its part of [B, Hkv, max_len, d]. */
+retopk_status paged_gather(const retopk_pages *c, int32_t dtype, int64_t n_tokens,
+                           const int32_t *seq, const int32_t *pos, retopk_rows k,
+                           retopk_rows v, void *stream);
+
+/* Bytes of workspace paged_attention needs for these arguments (0: none), or a negative
+ * retopk_status. */
+int64_t paged_attention_workspace(const retopk_pages *c, int64_t n_tokens, int32_t n_q_heads,
+                                  int64_t max_len, int64_t window);
+
+/* Full attention of single tokens over a paged cache: query row t attends the positions
+ * max(0, pos[t] - window + 1) .. pos[t] of sequence seq[t] (window = 0: from 0 on), so a
+ * step appends its rows and attends with the same seq and pos.  max_len is the host's bound
+ * of pos[t] + 1, which sizes the launch: positions from max_len on are left out, as are
+ * those without a page.  Scores are scaled by 1/sqrt(d); query head h uses KV head
+ * h / (n_q_heads / Hkv), and n_q_heads must be 1 to 8 times Hkv.  Writes out
+ * [n_tokens, n_q_heads, d] float32 and, when non-NULL, lse [n_tokens, n_q_heads] float32, the
+ * natural logarithm of the sum of e^score, with which parts of a context attended apart can
+ * be joined.  A row with no position left (seq outside [0, n_seqs), pos < 0, no page) gets
+ * out = 0 and lse = -infinity.  q, k and v must be finite.  workspace: 16-byte aligned device
+ * memory of at least paged_attention_workspace bytes (less: RETOPK_ERR_TOO_LARGE), used by this
+ * call only until its work on the stream is done; two graphs that may run at the same time
+ * need two. */
+retopk_status paged_attention(const retopk_pages *c, int32_t dtype, int64_t n_tokens,
+                              int32_t n_q_heads, const int32_t *seq, const int32_t *pos,
+                              retopk_rows q, int64_t max_len, int64_t window, float *out,
+                              float *lse, void *workspace, int64_t workspace_bytes,
+                              void *stream);
+
 const char *retopk_status_string(retopk_status s);
 
 #ifdef __cplusplus

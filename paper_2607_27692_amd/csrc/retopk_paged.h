@@ -1,0 +1,119 @@
+// retopk_paged.h -- shared by the paged-cache entry points (retopk_rope.hip,
+// retopk_attend.hip): their argument checks on the host, and on the device the place of
+// a position in the pages and the 4-bit format.  Not part of the public C ABI.
+#pragma once
+
+#include "retopk_device.h"
+#include "retopk_internal.h"
+#include "retopk_paged_plan.h"
+
+namespace retopk {
+
+constexpr int kGroup4 = 64;           // elements of a 4-bit row that share a scale and a mid
+
+// The pages as a kernel takes them.  A row's number is (page * Hkv + head) * page_size +
+// slot; check_pages keeps all of them below 2^31, so that only byte offsets need 64 bits.
+struct PagesArgs {
+    char *k, *v;
+    uint32_t *k_par, *v_par;
+    const int32_t *table;
+    int32_t n_kv_heads, page_size, n_pages, n_seqs, table_width;
+    Divisor by_page;
+};
+
+// Host checks (retopk_rope.hip), before any HIP call.
+retopk_status check_pages(const retopk_pages *c, int32_t dtype);
+PagesArgs pages_args(const retopk_pages &c);
+// Rows of `heads` heads of d elements of es bytes: pointer and strides 16-byte aligned,
+// strides not negative; for a tensor that is written, no two rows on each other.
+bool rows_ok(const retopk_rows &x, int64_t tokens, int64_t heads, int d, int es, bool written);
+
+// The number of the row that holds position p >= 0 of sequence s and KV head g, or -1.
+__device__ __forceinline__ int32_t row_of(const PagesArgs &c, int32_t s, int32_t p, int g)
+{
+    if (s < 0 || s >= c.n_seqs || p < 0) return -1;
+    const uint32_t at = divide((uint32_t)p, c.by_page);
+    if (at >= (uint32_t)c.table_width) return -1;
+    const int32_t page = c.table[(int64_t)s * c.table_width + at];
+    if (page < 0 || page >= c.n_pages) return -1;
+    return (page * c.n_kv_heads + g) * c.page_size + (p - (int32_t)at * c.page_size);
+}
+
+// bf16 bits of x, round to nearest even (finite x; NaN stays NaN in value, not in bits).
+__device__ __forceinline__ uint32_t bf16_bits(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (u >> 16) | 0x40u;
+    return (u + ((u >> 16) & 1u) + 0x7FFFu) >> 16;
+}
+
+// Elements of type T (float, or uint16_t for bf16) as 8 floats, and back.
+template <typename T> struct Oct;
+template <> struct Oct<float> {
+    u32x4_t a, b;
+    __device__ __forceinline__ void load(const float *p)
+    {
+        a = ((const u32x4_t *)p)[0];
+        b = ((const u32x4_t *)p)[1];
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = __uint_as_float(a[i]);
+            x[i + 4] = __uint_as_float(b[i]);
+        }
+    }
+    static __device__ __forceinline__ void store(float *p, const float (&x)[8])
+    {
+        u32x4_t u, v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u[i] = __float_as_uint(x[i]);
+            v[i] = __float_as_uint(x[i + 4]);
+        }
+        ((u32x4_t *)p)[0] = u;
+        ((u32x4_t *)p)[1] = v;
+    }
+    static __device__ __forceinline__ float one(const float *p) { return *p; }
+};
+template <> struct Oct<uint16_t> {
+    u32x4_t a;
+    __device__ __forceinline__ void load(const uint16_t *p) { a = *(const u32x4_t *)p; }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = bf16_lo(a[i]);
+            x[2 * i + 1] = bf16_hi(a[i]);
+        }
+    }
+    static __device__ __forceinline__ void store(uint16_t *p, const float (&x)[8])
+    {
+        u32x4_t u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = bf16_bits(x[2 * i]) | (bf16_bits(x[2 * i + 1]) << 16);
+        *(u32x4_t *)p = u;
+    }
+    static __device__ __forceinline__ float one(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
+};
+
+// The 8 values of a dword of 4-bit codes (elements 8 i .. 8 i + 7 of a row) of a group
+// with this parameter word.  c * scale is exact (4 and 8 bits), so the sum rounds once.
+__device__ __forceinline__ void values4(uint32_t codes, uint32_t par, float (&x)[8])
+{
+    const float scale = bf16_lo(par), mid = bf16_hi(par);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t w = codes >> (16 * h);
+        const uint32_t m[4] = {(w >> 4) & 7u, w & 7u, (w >> 12) & 7u, (w >> 8) & 7u};
+        const uint32_t s[4] = {(w >> 15) & 1u, (w >> 11) & 1u, (w >> 7) & 1u, (w >> 3) & 1u};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float c = (float)m[j] + 0.5f;
+            x[4 * h + j] = fmaf(scale, s[j] ? -c : c, mid);
+        }
+    }
+}
+
+}  // namespace retopk

@@ -13,6 +13,9 @@ import os
 from . import build as _build
 
 RETOPK_F32, RETOPK_BF16 = 0, 1
+RETOPK_PAGES_F32, RETOPK_PAGES_BF16, RETOPK_PAGES_Q4 = 0, 1, 2
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "ramp": 4}
+Q4_GROUP = 64               # elements of a 4-bit row that share a scale and a middle
 REUSE, FALLBACK, REFRESH, COLD = 0, 1, 2, 3
 PATH_NAMES = {REUSE: "reuse", FALLBACK: "fallback", REFRESH: "refresh", COLD: "cold"}
 STATUS = {0: "ok", -1: "invalid argument", -2: "unsupported shape", -3: "device out of memory",
@@ -26,7 +29,9 @@ EXPORTS = ("retopk_create", "retopk_destroy", "retopk_prefill_init", "retopk_dec
            "retopk_get_state",
            "retopk_set_state",
            "retopk_profile", "retopk_profile_read", "retopk_kernel_name",
-           "retopk_status_string")
+           "retopk_status_string",
+           "retopk_rope_init", "rotary_embed", "paged_append", "paged_gather",
+           "paged_attention_workspace", "paged_attention")
 
 
 class RetopkError(RuntimeError):
@@ -70,6 +75,27 @@ class retopk_debug(C.Structure):
                 ("n_cand", C.c_void_p), ("cand", C.c_void_p)]
 
 
+class retopk_pages(C.Structure):
+    _fields_ = [("format", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32), ("n_seqs", C.c_int32),
+                ("table_width", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_par", C.c_void_p), ("v_par", C.c_void_p), ("table", C.c_void_p)]
+
+
+class retopk_rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class retopk_rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("factor", C.c_double),
+                ("freq", C.c_double * 64)]
+
+
+class retopk_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("factor", C.c_double), ("original_len", C.c_double),
+                ("low", C.c_double), ("high", C.c_double)]
+
+
 _LIB = None
 
 
@@ -104,6 +130,17 @@ def load(path: str | None = None):
         "retopk_profile_read": ([P, I32, P, P], C.c_int),
         "retopk_kernel_name": ([I32], C.c_char_p),
         "retopk_status_string": ([C.c_int], C.c_char_p),
+        "retopk_rope_init": ([C.POINTER(retopk_rope), I32, I32, C.c_double,
+                              C.POINTER(retopk_rope_scaling)], C.c_int),
+        "rotary_embed": ([C.POINTER(retopk_rope), I32, I32, I32, I64, P, retopk_rows,
+                          retopk_rows, I32, P], C.c_int),
+        "paged_append": ([C.POINTER(retopk_pages), C.POINTER(retopk_rope), I32, I64, P, P,
+                          retopk_rows, retopk_rows, I32, retopk_rows, retopk_rows, P], C.c_int),
+        "paged_gather": ([C.POINTER(retopk_pages), I32, I64, P, P, retopk_rows, retopk_rows, P],
+                         C.c_int),
+        "paged_attention_workspace": ([C.POINTER(retopk_pages), I64, I32, I64, I64], I64),
+        "paged_attention": ([C.POINTER(retopk_pages), I32, I64, I32, P, P, retopk_rows, I64, I64,
+                             P, P, P, I64, P], C.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -267,6 +304,232 @@ def _check_io(fn: str, c: dict, q=None, k=None, v=None, out=None, sel=None, q_ta
     _check_tensor(fn, "out", out, bhq * d, 4)
     _check_tensor(fn, "sel", sel, bhq * c["k"], 4)
     _check_tensor(fn, "q_tail", q_tail, bhq * n_tail * d, es)
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions and the paged cache
+# ---------------------------------------------------------------------------
+
+def make_rope(rot_dim, theta=10000.0, interleaved=False, scaling="none", factor=1.0,
+              original_len=0, low=0.0, high=0.0) -> retopk_rope:
+    """Frequencies of a rotation (retopk_rope_init).  scaling: "none", "linear", "ntk",
+    "bands" or "ramp"; the last two take original_len and the turns low < high."""
+    if scaling not in ROPE_SCALINGS:
+        raise RetopkError("retopk_rope_init", -1, f"scaling {scaling!r}")
+    r = retopk_rope()
+    sc = retopk_rope_scaling(ROPE_SCALINGS[scaling], factor, original_len, low, high)
+    _check("retopk_rope_init", load().retopk_rope_init(C.byref(r), rot_dim, int(interleaved),
+                                                       theta, C.byref(sc)))
+    return r
+
+
+_NO_ROWS = retopk_rows(None, 0, 0)
+
+
+def _dtype_of(fn: str, name: str, x) -> int:
+    es = x.element_size()
+    if es == 4 and not str(x.dtype).endswith("int32"):
+        return RETOPK_F32
+    if es == 2 and not str(x.dtype).endswith("float16") or str(x.dtype).endswith("bfloat16"):
+        return RETOPK_BF16
+    raise RetopkError(fn, -1, f"{name} is {x.dtype}: float32 or bfloat16 expected")
+
+
+def _rows(fn: str, name: str, x, tokens=None, heads=None, d=None, like=None) -> retopk_rows:
+    """A [tokens, heads, d] GPU tensor whose last dimension is dense, of these sizes."""
+    if not x.is_cuda:
+        raise RetopkError(fn, -1, f"{name} is not a GPU tensor")
+    if x.dim() != 3:
+        raise RetopkError(fn, -1, f"{name} has {x.dim()} dimensions, [tokens, heads, d] expected")
+    want = tuple(a if b is None else b for a, b in zip(x.shape, (tokens, heads, d)))
+    if tuple(x.shape) != want:
+        raise RetopkError(fn, -1, f"{name} has shape {tuple(x.shape)}, {want} expected")
+    if like is not None and (x.dtype != like.dtype or x.device != like.device):
+        raise RetopkError(fn, -1, f"{name} is {x.dtype} on {x.device}, {like.dtype} on "
+                                  f"{like.device} expected")
+    ts, hs, es = x.stride()
+    if es != 1:
+        raise RetopkError(fn, -1, f"{name}: its last dimension is not dense")
+    # the stride of a dimension of one element is never used
+    return retopk_rows(x.data_ptr(), 0 if want[0] == 1 else ts, 0 if want[1] == 1 else hs)
+
+
+def _index(fn: str, name: str, x, n: int, like):
+    """A dense int32 GPU tensor of n elements on the device of `like`."""
+    if x.dtype.itemsize != 4 or x.is_floating_point():
+        raise RetopkError(fn, -1, f"{name} is {x.dtype}: int32 expected")
+    if x.device != like.device or not x.is_contiguous() or x.numel() != n:
+        raise RetopkError(fn, -1, f"{name}: {n} dense elements on {like.device} expected")
+    return x.data_ptr()
+
+
+def _launch(name: str, device, stream, *args):
+    """Calls a library function with the device of its tensors current."""
+    import torch
+    fn = getattr(load(), name)
+    if device.index == torch.cuda.current_device():
+        _check(name, fn(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(name, fn(*args, _stream(stream)))
+
+
+def rotary_embed(rope: retopk_rope, x, pos, out, inverse=False, stream=None) -> None:
+    """out = x [tokens, heads, d] rotated to the int32 positions pos [tokens]; with inverse,
+    the gradient of x for the gradient x of out.  out may be x."""
+    rx = _rows("rotary_embed", "x", x)
+    t, h, d = x.shape
+    ro = _rows("rotary_embed", "out", out, t, h, d, x)
+    _launch("rotary_embed", x.device, stream, C.byref(rope), _dtype_of("rotary_embed", "x", x), d,
+            h, t, _index("rotary_embed", "pos", pos, t, x), rx, ro, 1 if inverse else 0)
+
+
+class PagedCache:
+    """Pages of keys and values and the table that maps positions to them
+    (include/retopk.h, retopk_pages).  k, v: [n_pages, Hkv, page_size, d] float32 or bfloat16,
+    or [n_pages, Hkv, page_size, d / 2] uint8 with k_par, v_par [n_pages, Hkv, page_size, d / 64]
+    int32 for 4-bit rows; table: [n_seqs, table_width] int32.  The tensors stay the
+    caller's: pages are added by writing their ids into the table."""
+
+    def __init__(self, k, v, table, k_par=None, v_par=None):
+        fn = "retopk_pages"
+        if k.dim() != 4 or table.dim() != 2:
+            raise RetopkError(fn, -1, "k: 4 dimensions, table: 2 expected")
+        self.q4 = k.element_size() == 1
+        n, hkv, page, d = k.shape
+        if self.q4:
+            d *= 2
+            if k_par is None or v_par is None:
+                raise RetopkError(fn, -1, "4-bit pages need k_par and v_par")
+        per = {"k": (k, k.shape), "v": (v, k.shape), "table": (table, table.shape)}
+        if self.q4:
+            per["k_par"] = (k_par, (n, hkv, page, d // Q4_GROUP))
+            per["v_par"] = (v_par, (n, hkv, page, d // Q4_GROUP))
+        for name, (x, shape) in per.items():
+            if not x.is_cuda or x.device != k.device or not x.is_contiguous():
+                raise RetopkError(fn, -1, f"{name}: a dense tensor on {k.device} expected")
+            if tuple(x.shape) != tuple(shape):
+                raise RetopkError(fn, -1, f"{name} has shape {tuple(x.shape)}, {tuple(shape)} expected")
+        if v.dtype != k.dtype:
+            raise RetopkError(fn, -1, f"v is {v.dtype}, {k.dtype} expected")
+        for name in ("table", "k_par", "v_par"):
+            if name in per and (per[name][0].element_size() != 4 or
+                                per[name][0].is_floating_point()):
+                raise RetopkError(fn, -1, f"{name}: int32 expected")
+        fmt = RETOPK_PAGES_Q4 if self.q4 else {RETOPK_F32: RETOPK_PAGES_F32,
+                                               RETOPK_BF16: RETOPK_PAGES_BF16}[_dtype_of(fn, "k", k)]
+        self.tensors = (k, v, table, k_par, v_par)
+        self.k, self.device, self.n_kv_heads, self.head_dim = k, k.device, hkv, d
+        self.c = retopk_pages(fmt, hkv, d, page, n, table.shape[0], table.shape[1], k.data_ptr(),
+                              v.data_ptr(), k_par.data_ptr() if self.q4 else None,
+                              v_par.data_ptr() if self.q4 else None, table.data_ptr())
+
+    @staticmethod
+    def allocate(fmt, n_pages, n_kv_heads, page_size, head_dim, n_seqs, table_width,
+                 device="cuda") -> "PagedCache":
+        """A cache of empty pages; fmt: "f32", "bf16" or "q4".  No sequence has a page yet
+        (the table holds -1)."""
+        import torch
+        shape, dev = (n_pages, n_kv_heads, page_size), dict(device=device)
+        table = torch.full((n_seqs, table_width), -1, dtype=torch.int32, **dev)
+        if fmt == "q4":
+            k, v = (torch.zeros((*shape, head_dim // 2), dtype=torch.uint8, **dev)
+                    for _ in range(2))
+            kp, vp = (torch.zeros((*shape, head_dim // Q4_GROUP), dtype=torch.int32, **dev)
+                      for _ in range(2))
+            return PagedCache(k, v, table, kp, vp)
+        dt = {"f32": torch.float32, "bf16": torch.bfloat16}[fmt]
+        k, v = (torch.zeros((*shape, head_dim), dtype=dt, **dev) for _ in range(2))
+        return PagedCache(k, v, table)
+
+    @property
+    def table(self):
+        return self.tensors[2]
+
+    def workspace(self, n_tokens, n_q_heads, max_len, window=0):
+        """A workspace for paged_attention calls of these sizes, None where it needs none."""
+        import torch
+        n = paged_attention_workspace(self, n_tokens, n_q_heads, max_len, window)
+        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+
+
+def paged_append(cache: PagedCache, seq, pos, k, v, rope: retopk_rope | None = None, q=None,
+                 q_out=None, stream=None) -> None:
+    """Rows t of k and v [tokens, Hkv, d] to positions pos[t] of sequences seq[t], k rotated on
+    the way when rope is given; q [tokens, Hq, d], rotated, to q_out."""
+    fn = "paged_append"
+    rk = _rows(fn, "k", k, None, cache.n_kv_heads, cache.head_dim)
+    t = k.shape[0]
+    rv = _rows(fn, "v", v, t, cache.n_kv_heads, cache.head_dim, k)
+    hq, rq, ro = 0, _NO_ROWS, _NO_ROWS
+    if q is not None:
+        if q_out is None:
+            raise RetopkError(fn, -1, "q without q_out")
+        rq = _rows(fn, "q", q, t, None, cache.head_dim, k)
+        hq = q.shape[1]
+        ro = _rows(fn, "q_out", q_out, t, hq, cache.head_dim, k)
+    if k.device != cache.device:
+        raise RetopkError(fn, -1, f"k is on {k.device}, the cache on {cache.device}")
+    _launch(fn, k.device, stream, C.byref(cache.c), C.byref(rope) if rope is not None else None,
+            _dtype_of(fn, "k", k), t, _index(fn, "seq", seq, t, k), _index(fn, "pos", pos, t, k),
+            rk, rv, hq, rq, ro)
+
+
+def paged_gather(cache: PagedCache, seq, pos, k=None, v=None, stream=None) -> None:
+    """Positions pos[t] of sequences seq[t] read into rows t of k and v [tokens, Hkv, d]."""
+    fn = "paged_gather"
+    first = k if k is not None else v
+    if first is None:
+        return
+    t, h, d = seq.numel(), cache.n_kv_heads, cache.head_dim
+    if first.device != cache.device:
+        raise RetopkError(fn, -1, f"k or v is on {first.device}, the cache on {cache.device}")
+    rk = _rows(fn, "k", k, t, h, d) if k is not None else _NO_ROWS
+    rv = _rows(fn, "v", v, t, h, d, first) if v is not None else _NO_ROWS
+    _launch(fn, first.device, stream, C.byref(cache.c), _dtype_of(fn, "k", first), t,
+            _index(fn, "seq", seq, t, first), _index(fn, "pos", pos, t, first), rk, rv)
+
+
+def paged_attention_workspace(cache: PagedCache, n_tokens, n_q_heads, max_len, window=0) -> int:
+    """Bytes of workspace that paged_attention needs."""
+    n = load().paged_attention_workspace(C.byref(cache.c), n_tokens, n_q_heads, max_len, window)
+    if n < 0:
+        _check("paged_attention_workspace", n)
+    return n
+
+
+def _workspace_on(cache: PagedCache, t, hq, max_len, window, stream):
+    """A workspace of the call's own, whose memory the allocator ties to its stream."""
+    import torch
+    if stream is None:
+        return cache.workspace(t, hq, max_len, window)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=cache.device)
+    with torch.cuda.stream(stream):
+        return cache.workspace(t, hq, max_len, window)
+
+
+def paged_attention(cache: PagedCache, seq, pos, q, out, max_len, window=0, lse=None,
+                    workspace=None, stream=None) -> None:
+    """Row t of q [tokens, Hq, d] attends the positions up to pos[t] of sequence seq[t]; out
+    [tokens, Hq, d] and lse [tokens, Hq] are float32.  workspace: PagedCache.workspace of the
+    same sizes (None: a new one; hold one for graphs, and one a graph)."""
+    fn = "paged_attention"
+    rq = _rows(fn, "q", q, None, None, cache.head_dim)
+    t, hq = q.shape[0], q.shape[1]
+    if q.device != cache.device:
+        raise RetopkError(fn, -1, f"q is on {q.device}, the cache on {cache.device}")
+    for name, x, n in (("out", out, t * hq * cache.head_dim), ("lse", lse, t * hq)):
+        if x is not None:
+            _check_tensor(fn, name, x, n, 4)
+            if not x.is_floating_point() or x.device != q.device:
+                raise RetopkError(fn, -1, f"{name}: float32 on {q.device} expected")
+    if workspace is None:
+        workspace = _workspace_on(cache, t, hq, max_len, window, stream)
+    _launch(fn, q.device, stream, C.byref(cache.c), _dtype_of(fn, "q", q), t, hq,
+            _index(fn, "seq", seq, t, q), _index(fn, "pos", pos, t, q), rq, max_len, window,
+            out.data_ptr(), _addr(lse), _addr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
 # ---------------------------------------------------------------------------
