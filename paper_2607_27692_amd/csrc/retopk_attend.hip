@@ -12,6 +12,7 @@ namespace retopk {
 namespace {
 
 constexpr int kAttendThreads = 256;
+constexpr float kLn2 = 0.69314718055994530942f;
 
 struct AttendArgs {
     PagesArgs c;
@@ -21,10 +22,10 @@ struct AttendArgs {
     int32_t n_q, group;        // query heads; of a KV head
     int32_t max_len, window;
     int32_t chunk_rows, chunks;
-    float inv_sqrt_d;
+    float scale2;              // log2(e) / sqrt(d): scores are in powers of two
     float *out, *lse;          // chunks == 1
     float *part_o;             // else [tokens * n_q, chunks, d]
-    float2 *part_ml;           // [tokens * n_q, chunks]: maximum, sum
+    float2 *part_ml;           // [tokens * n_q, chunks]: maximum (a power of two), sum
 };
 
 // The attended positions [first, len) of a token, len = 0 where there are none; chunk c
@@ -49,7 +50,7 @@ __device__ __forceinline__ void write_result(const AttendArgs &a, int64_t row, i
 {
     if (a.chunks == 1) {
         a.out[row * d + e] = l > 0.0f ? o / l : 0.0f;
-        if (e == 0 && a.lse) a.lse[row] = l > 0.0f ? m + logf(l) : -INFINITY;
+        if (e == 0 && a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
     } else {
         a.part_o[(row * a.chunks + chunk) * d + e] = o;
         if (e == 0) a.part_ml[row * a.chunks + chunk] = make_float2(m, l);
@@ -106,8 +107,8 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend(AttendArgs a)
             for (int i = 0; i < 8; ++i) s = fmaf(q[j][i], k[i], s);
 #pragma unroll
             for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
-            s *= a.inv_sqrt_d;
-            const float mn = fmaxf(m[j], s), f = expf(m[j] - mn), p = expf(s - mn);
+            s *= a.scale2;
+            const float mn = fmaxf(m[j], s), f = exp2f(m[j] - mn), p = exp2f(s - mn);
             m[j] = mn;
             l[j] = l[j] * f + p;
 #pragma unroll
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend(AttendArgs a)
 #pragma unroll
         for (int o = LPR; o < 64; o <<= 1) {
             const float m2 = __shfl_xor(m[j], o), l2 = __shfl_xor(l[j], o), mn = fmaxf(m[j], m2);
-            const float f = expf(m[j] - mn), f2 = expf(m2 - mn);
+            const float f = exp2f(m[j] - mn), f2 = exp2f(m2 - mn);
             m[j] = mn;
             l[j] = l[j] * f + l2 * f2;
 #pragma unroll
@@ -141,7 +142,320 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend(AttendArgs a)
         for (int w = 1; w < NW; ++w) mx = fmaxf(mx, s_m[w][j]);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float f = expf(s_m[w][j] - mx);
+            const float f = exp2f(s_m[w][j] - mx);
+            o += f * s_o[w][j][e];
+            ls += f * s_l[w][j];
+        }
+        write_result(a, t * a.n_q + g * a.group + j, chunk, D, e, o, mx, ls);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// 4-bit pages
+// ---------------------------------------------------------------------------
+
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+// Codes as operands of the matrix cores: in a half-word (b0 low, b1 high byte) the sign of
+// code 0 is bit 15 and its magnitude bits 4 .. 6, which with bit 3 set is the subnormal
+// float16 c * 2^-20, exact; code 1 lies four bits lower, codes 2 and 3 the same with the
+// bytes swapped.  One and-or a pair of codes, no conversion.
+constexpr int kCodeExp = 20;
+__device__ __forceinline__ uint32_t code_pair(uint32_t x) { return (x & 0x80708070u) | 0x00080008u; }
+__device__ __forceinline__ void code_quad(uint32_t x, uint32_t (&r)[4])
+{
+    const uint32_t y = __builtin_amdgcn_perm(x, x, 0x02030001u);
+    r[0] = code_pair(x);
+    r[1] = code_pair(x << 4);
+    r[2] = code_pair(y);
+    r[3] = code_pair(y << 4);
+}
+
+// Base rows of the two 16-position halves of a tile: a 4-bit page holds whole halves, so
+// that a half has one page, looked up once for the wave.
+struct Half {
+    int32_t row;               // of its first position; 0 where it has no page
+    bool there;
+};
+__device__ __forceinline__ Half half_of(const PagesArgs &c, const int32_t *table, int32_t pos, int g)
+{
+    const uint32_t at = divide((uint32_t)pos, c.by_page);
+    int32_t page = -1;
+    if (at < (uint32_t)c.table_width)
+        page = ((const __attribute__((address_space(4))) int32_t *)(uintptr_t)table)[at];
+    const bool there = page >= 0 && page < c.n_pages;
+    return Half{there ? (page * c.n_kv_heads + g) * c.page_size + (pos - (int32_t)at * c.page_size) : 0, there};
+}
+
+// k_attend4: each wave streams its own 32-position tiles.  Matrix columns are (group of 64
+// elements, head): column c has head c % 8 and, for d = 128, group c / 8, its query zero
+// outside that group, so that a product's result is a group's sum of codes times query and
+// every lane applies one scale and mid.  The weights times the value scales are the second
+// product's other operand, in two float16 parts (22 bits) of which a common power of two,
+// kept above every scale met so far, is taken out; value codes are exact.
+template <typename T, int D>
+__global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
+{
+    constexpr int NW = kAttendThreads / 64, NG = D / kGroup4;
+    constexpr int KD = D / 32;                 // code dwords of a lane's share of a key row
+    constexpr int NV = D / 16;                 // value products: codes of a lane's share of a row
+    constexpr int NQ = sizeof(T) == 4 ? 2 : 1; // float16 parts of the query
+    __shared__ float s_m[NW][8], s_l[NW][8], s_o[NW][8][D];
+    const int chunk = blockIdx.x % a.chunks, bg = blockIdx.x / a.chunks;
+    const int g = bg % a.c.n_kv_heads;
+    const int64_t t = bg / a.c.n_kv_heads;
+    const int32_t sq = a.seq[t];
+    const Span sp = span_of(a, sq, a.pos[t]);
+    const int lo = sp.base + chunk * a.chunk_rows, hi = min(sp.len, lo + a.chunk_rows);
+    if (lo >= hi && !(chunk == 0 && a.chunks == 1)) return;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int gr = NG == 2 ? col >> 3 : 0, head = (col & 7) < a.group ? (col & 7) : 0;
+    const int n_it = (hi - lo + 32 * NW - 1 - 32 * wave) / (32 * NW);
+    const int32_t *table = a.c.table + (int64_t)(sq < 0 ? 0 : sq) * a.c.table_width;
+
+    // the query, scaled by a power of two to [2^14, 2^15): bf16 fits one float16 part, f32 two
+    f16x8_t qb[NQ][KD];
+    int q_exp;
+    float q_sum = 0.0f;
+    {
+        float x[KD][8], top = 0.0f;
+        const T *qr = (const T *)a.q + t * a.q_ts + (g * a.group + head) * a.q_hs + kq * (D / 4);
+#pragma unroll
+        for (int i = 0; i < KD; ++i) {
+            Oct<T> v;
+            v.load(qr + 8 * i);
+            v.get(x[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
+        }
+        top = max_rows_f32(top);
+        q_exp = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) - 15 : 0;
+        const bool mine = NG == 1 || (kq >> 1) == gr;
+#pragma unroll
+        for (int i = 0; i < KD; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                // code order: elements j and j + 4 in register j
+                const float y = mine ? ldexpf(x[i][(e >> 1) + 4 * (e & 1)], -q_exp) : 0.0f;
+                q_sum += y;
+                const _Float16 h = (_Float16)y;
+                qb[0][i][e] = h;
+                if constexpr (NQ == 2) qb[1][i][e] = (_Float16)(y - (float)h);
+            }
+        q_sum = add16_f32(q_sum, q_sum);
+        q_sum = ldexpf(add32_f32(q_sum, q_sum), -kCodeExp);
+    }
+    const int s_exp = q_exp + kCodeExp;
+
+    u32x4_t kc[2];             // key codes: the row's dwords kq * KD ..
+    uint32_t kp[8], vp[8], vc[8];
+    Half h0[2], h1[2];         // this tile's halves, the next one's
+    auto halves = [&](int it, Half (&h)[2]) {
+        const int r = lo + (it * NW + wave) * 32;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) h[u] = half_of(a.c, table, r + 16 * u, g);
+    };
+    auto load_k = [&](const Half (&h)[2]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const char *p = a.c.k + (int64_t)(h[u].row + col) * (D / 2) + kq * (D / 8);
+            if constexpr (KD == 4) {
+                kc[u] = *(const u32x4_t *)p;
+            } else {
+                const uint2 x = *(const uint2 *)p;
+                kc[u][0] = x.x;
+                kc[u][1] = x.y;
+            }
+        }
+    };
+    auto load_par = [&](const Half (&h)[2], const uint32_t *par, uint32_t (&w)[8]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t *p = par + (int64_t)(h[u].row + 4 * kq) * NG + gr;
+            if constexpr (NG == 1) {
+                const u32x4_t x = *(const u32x4_t *)p;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[4 * u + i] = x[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[4 * u + i] = p[i * NG];
+            }
+        }
+    };
+    auto load_v = [&](const Half (&h)[2]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const char *p = a.c.v + (int64_t)(h[u].row + 4 * kq) * (D / 2) + col * (D / 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (D == 128) vc[4 * u + i] = *(const uint32_t *)(p + i * (D / 2));
+                else vc[4 * u + i] = *(const uint16_t *)(p + i * (D / 2));
+            }
+        }
+    };
+
+    f32x4_t acc[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = -FLT_MAX, l = 0.0f, z = 0.0f, limit = 0.0f;
+    int v_exp = 0;
+
+    auto tile = [&](int it, const Half (&h)[2], const Half (&hn)[2], auto more) {
+        float s[8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f32x4_t d = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < KD; ++i) {
+                uint32_t r[4];
+                code_quad(kc[u][i], r);
+                const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[0], r[1], r[2], r[3]});
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qb[n][i], d, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[4 * u + i] = d[i];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(more)::value) load_k(hn);
+        __builtin_amdgcn_sched_barrier(0);
+        const int row = lo + (it * NW + wave) * 32;
+        const bool whole = row >= sp.first && row + 32 <= hi && h[0].there && h[1].there;
+        float tm = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float x = fmaf(bf16_lo(kp[i]), s[i], bf16_hi(kp[i]) * q_sum);
+            if constexpr (NG == 2) x += row_ror_f32(x, 8);       // the other group of the row
+            s[i] = ldexpf(x, s_exp) * a.scale2;
+        }
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = row + 16 * (i >> 2) + 4 * kq + (i & 3);
+                const bool on = r >= sp.first && r < hi && h[i >> 2].there;
+                s[i] = on ? s[i] : -INFINITY;
+                vp[i] = on ? vp[i] : 0u;                         // whatever lies there: weight and value 0
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tm = fmaxf(tm, s[i]);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(more)::value) load_par(hn, a.c.k_par, kp);
+        __builtin_amdgcn_sched_barrier(0);
+        const float mn = fmaxf(m, max_rows_f32(tm));
+        const float f = __builtin_amdgcn_exp2f(m - mn);
+        const bool moved = __ballot(mn != m) != 0ull;
+        m = mn;
+        float top = 0.0f, vs[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(s[i] - mn);
+            vs[i] = bf16_lo(vp[i]);
+            top = fmaxf(top, vs[i]);
+        }
+        if (moved) {
+            l *= f;
+            z *= f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) acc[j] *= f;
+        }
+        // a scale past the limit: the power of two moves, with two bits to spare
+        if (__ballot(top >= limit) != 0ull && __ballot(top > 0.0f) != 0ull) {
+            float w = max_rows_f32(top);
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) w = fmaxf(w, __shfl_xor(w, o));
+            const int e = __builtin_amdgcn_frexp_expf(w) + 2;     // every scale below 2^(e - 2)
+            const int n = 15 - e;
+            if (limit > 0.0f)
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[j][i] = ldexpf(acc[j][i], n - v_exp);
+            v_exp = n;
+            limit = ldexpf(1.0f, e);
+        }
+        uint32_t ph[4], pl[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = s[2 * i] * ldexpf(vs[2 * i], v_exp), y = s[2 * i + 1] * ldexpf(vs[2 * i + 1], v_exp);
+            const f16x2_t hx = {(_Float16)x, (_Float16)y};
+            const f16x2_t lx = {(_Float16)(x - (float)hx[0]), (_Float16)(y - (float)hx[1])};
+            ph[i] = __builtin_bit_cast(uint32_t, hx);
+            pl[i] = __builtin_bit_cast(uint32_t, lx);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z = fmaf(s[i], bf16_hi(vp[i]), z);
+        l += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(more)::value) load_par(hn, a.c.v_par, vp);
+        __builtin_amdgcn_sched_barrier(0);
+        const f16x8_t bh = __builtin_bit_cast(f16x8_t, u32x4_t{ph[0], ph[1], ph[2], ph[3]});
+        const f16x8_t bl = __builtin_bit_cast(f16x8_t, u32x4_t{pl[0], pl[1], pl[2], pl[3]});
+#pragma unroll
+        for (int w = 0; w < NV / 4; ++w) {
+            uint32_t r[4][4];                                    // [code][pair of positions]
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], w ? 0x07060302u : 0x05040100u);
+                const uint32_t y = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], w ? 0x06070203u : 0x04050001u);
+                r[0][i] = code_pair(x);
+                r[1][i] = code_pair(x << 4);
+                r[2][i] = code_pair(y);
+                r[3][i] = code_pair(y << 4);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[j][0], r[j][1], r[j][2], r[j][3]});
+                acc[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, bh, acc[4 * w + j], 0, 0, 0);
+                acc[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, bl, acc[4 * w + j], 0, 0, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(more)::value) load_v(hn);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (n_it > 0) {
+        halves(0, h0);
+        load_k(h0);
+        load_par(h0, a.c.k_par, kp);
+        load_par(h0, a.c.v_par, vp);
+        load_v(h0);
+        for (int it = 0; it + 1 < n_it; ++it) {
+            halves(it + 1, h1);
+            tile(it, h0, h1, std::true_type{});
+            h0[0] = h1[0];
+            h0[1] = h1[1];
+        }
+        tile(n_it - 1, h0, h0, std::false_type{});
+    }
+    l = add16_f32(l, l);
+    l = add32_f32(l, l);
+    z = add16_f32(z, z);
+    z = add32_f32(z, z);
+    if (lane < 8) {
+        s_m[wave][lane] = m;
+        s_l[wave][lane] = l;
+    }
+    // rows 4 kq + i of product j are elements (4 kq + i) * (D / 16) + j, right in the columns of
+    // their own group
+    if (col < 8 * NG && (NG == 1 || (kq >> 1) == gr)) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                s_o[wave][col & 7][(4 * kq + i) * (D / 16) + j] = ldexpf(acc[j][i], kCodeExp - v_exp) + z;
+    }
+    __syncthreads();
+    for (int i = tid; i < a.group * D; i += kAttendThreads) {
+        const int j = i / D, e = i % D;
+        float mx = s_m[0][j], o = 0.0f, ls = 0.0f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) mx = fmaxf(mx, s_m[w][j]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = __builtin_amdgcn_exp2f(s_m[w][j] - mx);
             o += f * s_o[w][j][e];
             ls += f * s_l[w][j];
         }
@@ -166,7 +480,7 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend_merge(AttendArgs a)
     float o = 0.0f, l = 0.0f;
     for (int c = part; c < nch; c += P) {
         const float2 x = ml[c];
-        const float f = expf(x.x - m);
+        const float f = exp2f(x.x - m);
         l = fmaf(f, x.y, l);
         o = fmaf(f, a.part_o[(row * a.chunks + c) * D + e], o);
     }
@@ -180,7 +494,7 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend_merge(AttendArgs a)
             l += s_l[p];
         }
         a.out[row * D + e] = l > 0.0f ? o / l : 0.0f;
-        if (e == 0 && a.lse) a.lse[row] = l > 0.0f ? m + logf(l) : -INFINITY;
+        if (e == 0 && a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
     }
 }
 
@@ -193,8 +507,7 @@ template <int D> const void *attend_kernel(int format, int dtype, int group)
 {
     if (format == RETOPK_PAGES_BF16) return attend_kernel<uint16_t, D, RETOPK_PAGES_BF16>(group);
     if (format == RETOPK_PAGES_F32) return attend_kernel<float, D, RETOPK_PAGES_F32>(group);
-    return dtype == RETOPK_BF16 ? attend_kernel<uint16_t, D, RETOPK_PAGES_Q4>(group)
-                                : attend_kernel<float, D, RETOPK_PAGES_Q4>(group);
+    return dtype == RETOPK_BF16 ? (const void *)&k_attend4<uint16_t, D> : (const void *)&k_attend4<float, D>;
 }
 
 // Checks the arguments the workspace depends on and makes the plan.
@@ -260,7 +573,7 @@ retopk_status paged_attention(const retopk_pages *c, int32_t dtype, int64_t n_to
     a.window = window <= rows ? (int32_t)window : 0;
     a.chunk_rows = (int32_t)p.chunk_rows;
     a.chunks = (int32_t)p.chunks;
-    a.inv_sqrt_d = (float)(1.0 / __builtin_sqrt((double)d));
+    a.scale2 = (float)(1.44269504088896340736 / __builtin_sqrt((double)d));
     a.out = out;
     a.lse = lse;
     a.part_o = (float *)workspace;
