@@ -154,6 +154,7 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend(AttendArgs a)
 // 4-bit pages
 // ---------------------------------------------------------------------------
 
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
@@ -162,7 +163,13 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 // float16 c * 2^-20, exact; code 1 lies four bits lower, codes 2 and 3 the same with the
 // bytes swapped.  One and-or a pair of codes, no conversion.
 constexpr int kCodeExp = 20;
-__device__ __forceinline__ uint32_t code_pair(uint32_t x) { return (x & 0x80708070u) | 0x00080008u; }
+__device__ __forceinline__ uint32_t code_pair(uint32_t x)
+{
+    // (x & 0x80708070) | 0x00080008; the compiler makes two instructions of it
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(0x80708070u), "v"(0x00080008u));
+    return r;
+}
 __device__ __forceinline__ void code_quad(uint32_t x, uint32_t (&r)[4])
 {
     const uint32_t y = __builtin_amdgcn_perm(x, x, 0x02030001u);
@@ -188,19 +195,29 @@ __device__ __forceinline__ Half half_of(const PagesArgs &c, const int32_t *table
     return Half{there ? (page * c.n_kv_heads + g) * c.page_size + (pos - (int32_t)at * c.page_size) : 0, there};
 }
 
-// k_attend4: each wave streams its own 32-position tiles.  Matrix columns are (group of 64
-// elements, head): column c has head c % 8 and, for d = 128, group c / 8, its query zero
-// outside that group, so that a product's result is a group's sum of codes times query and
-// every lane applies one scale and mid.  The weights times the value scales are the second
-// product's other operand, in two float16 parts (22 bits) of which a common power of two,
-// kept above every scale met so far, is taken out; value codes are exact.
-template <typename T, int D>
-__global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
+// k_attend4: each wave streams its own 32-position tiles.  A matrix column is (half of the
+// tile, group of 64 elements, query head), as far as eight columns a half suffice (PACK: d = 64,
+// or up to 4 heads of d = 128), else (group, head).  The query is zero outside a column's group, so
+// that a product's result is one group's sum of codes times query, to which a lane applies one
+// scale and mid: V scores a lane, V = 4 or 8.  The weights times the value scales are the second
+// product's other operand, in two float16 parts (24 bits together) of which a common power of
+// two, kept above every scale met so far, is taken out; value codes are exact.
+//
+// What the matrix cores round has a bias (against float64 the outputs of 128K rows were 1.2e-5 off
+// with plain accumulation, 2.5e-7 so): products are cut below 2^-24 of the largest, and a sum that
+// does not fit 24 bits rounds to one side.  The high parts are therefore whole numbers, whose
+// products are multiples of 2^-21 and sum exactly, kFlush tiles long, until the vector units
+// add them to acc; the low parts' sums, 2^-12 the size, may be biased.
+constexpr int kFlush = 4;
+template <typename T, int D, bool PACK>
+__global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
 {
     constexpr int NW = kAttendThreads / 64, NG = D / kGroup4;
+    constexpr int V = PACK ? 4 : 8;            // positions a lane weighs in a tile
     constexpr int KD = D / 32;                 // code dwords of a lane's share of a key row
     constexpr int NV = D / 16;                 // value products: codes of a lane's share of a row
     constexpr int NQ = sizeof(T) == 4 ? 2 : 1; // float16 parts of the query
+    static_assert(PACK || NG == 2, "d = 64 always packs");
     __shared__ float s_m[NW][8], s_l[NW][8], s_o[NW][8][D];
     const int chunk = blockIdx.x % a.chunks, bg = blockIdx.x / a.chunks;
     const int g = bg % a.c.n_kv_heads;
@@ -211,7 +228,11 @@ __global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
     if (lo >= hi && !(chunk == 0 && a.chunks == 1)) return;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int gr = NG == 2 ? col >> 3 : 0, head = (col & 7) < a.group ? (col & 7) : 0;
+    // group and head of this lane's column; packed columns 4 .. 7 of d = 128 count the heads down,
+    // so that a half-row mirror meets the other group of the same head
+    const int c8 = col & 7, upper = PACK ? col >> 3 : 0;
+    const int gr = NG == 1 ? 0 : PACK ? c8 >> 2 : col >> 3;
+    const int hc = PACK && NG == 2 ? (gr ? 7 - c8 : c8) : c8, head = hc < a.group ? hc : 0;
     const int n_it = (hi - lo + 32 * NW - 1 - 32 * wave) / (32 * NW);
     const int32_t *table = a.c.table + (int64_t)(sq < 0 ? 0 : sq) * a.c.table_width;
 
@@ -247,33 +268,40 @@ __global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
         q_sum = add16_f32(q_sum, q_sum);
         q_sum = ldexpf(add32_f32(q_sum, q_sum), -kCodeExp);
     }
-    const int s_exp = q_exp + kCodeExp;
+    // scores in powers of two are the products times this factor; what it cannot hold of the
+    // exponent (queries past 2^94 or below 2^-106) is applied apart
+    const int s_exp = q_exp + kCodeExp, s_near = min(max(s_exp, -100), 100);
+    const float s_mul = ldexpf(a.scale2, s_near);
+    const bool far = __ballot(s_exp != s_near) != 0ull;
 
     u32x4_t kc[2];             // key codes: the row's dwords kq * KD ..
-    uint32_t kp[8], vp[8], vc[8];
+    uint32_t kp[V], vp[V], vc[8];
     Half h0[2], h1[2];         // this tile's halves, the next one's
     auto halves = [&](int it, Half (&h)[2]) {
         const int r = lo + (it * NW + wave) * 32;
 #pragma unroll
         for (int u = 0; u < 2; ++u) h[u] = half_of(a.c, table, r + 16 * u, g);
     };
+    // a half's base is the wave's own, a lane's offset in it the same for every half
+    const uint32_t k_off = col * (D / 2) + kq * (D / 8), v_off = 4 * kq * (D / 2) + col * (D / 32);
     auto load_k = [&](const Half (&h)[2]) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const char *p = a.c.k + (int64_t)(h[u].row + col) * (D / 2) + kq * (D / 8);
+            const char *p = a.c.k + (int64_t)h[u].row * (D / 2);
             if constexpr (KD == 4) {
-                kc[u] = *(const u32x4_t *)p;
+                kc[u] = *(const u32x4_t *)(p + k_off);
             } else {
-                const uint2 x = *(const uint2 *)p;
+                const uint2 x = *(const uint2 *)(p + k_off);
                 kc[u][0] = x.x;
                 kc[u][1] = x.y;
             }
         }
     };
-    auto load_par = [&](const Half (&h)[2], const uint32_t *par, uint32_t (&w)[8]) {
+    auto load_par = [&](const Half (&h)[2], const uint32_t *par, uint32_t (&w)[V]) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint32_t *p = par + (int64_t)(h[u].row + 4 * kq) * NG + gr;
+        for (int u = 0; u < V / 4; ++u) {
+            const int32_t row = (PACK ? (upper ? h[1].row : h[0].row) : h[u].row) + 4 * kq;
+            const uint32_t *p = par + (int64_t)row * NG + gr;
             if constexpr (NG == 1) {
                 const u32x4_t x = *(const u32x4_t *)p;
 #pragma unroll
@@ -287,36 +315,47 @@ __global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
     auto load_v = [&](const Half (&h)[2]) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const char *p = a.c.v + (int64_t)(h[u].row + 4 * kq) * (D / 2) + col * (D / 32);
+            const char *p = a.c.v + (int64_t)h[u].row * (D / 2);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if constexpr (D == 128) vc[4 * u + i] = *(const uint32_t *)(p + i * (D / 2));
-                else vc[4 * u + i] = *(const uint16_t *)(p + i * (D / 2));
+                if constexpr (D == 128) vc[4 * u + i] = *(const uint32_t *)(p + v_off + i * (D / 2));
+                else vc[4 * u + i] = *(const uint16_t *)(p + v_off + i * (D / 2));
             }
         }
     };
 
-    f32x4_t acc[NV];
+    // sums of the high parts (exact, and what they were flushed to) and of the low parts
+    f32x4_t run[NV], acc[NV], low[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < NV; ++j) run[j] = acc[j] = low[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    auto flush = [&]() {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            acc[j] += run[j];
+            run[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    };
     float m = -FLT_MAX, l = 0.0f, z = 0.0f, limit = 0.0f;
     int v_exp = 0;
 
     auto tile = [&](int it, const Half (&h)[2], const Half (&hn)[2], auto more) {
-        float s[8];
+        float s[V];
+        {
+            f32x4_t d[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            f32x4_t d = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int u = 0; u < 2; ++u) {
+                d[u] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int i = 0; i < KD; ++i) {
-                uint32_t r[4];
-                code_quad(kc[u][i], r);
-                const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[0], r[1], r[2], r[3]});
+                for (int i = 0; i < KD; ++i) {
+                    uint32_t r[4];
+                    code_quad(kc[u][i], r);
+                    const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[0], r[1], r[2], r[3]});
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qb[n][i], d, 0, 0, 0);
+                    for (int n = NQ - 1; n >= 0; --n) d[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qb[n][i], d[u], 0, 0, 0);
+                }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[4 * u + i] = d[i];
+            for (int i = 0; i < V; ++i) s[i] = PACK ? (upper ? d[1][i & 3] : d[0][i & 3]) : d[i >> 2][i & 3];
         }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(more)::value) load_k(hn);
@@ -325,41 +364,53 @@ __global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
         const bool whole = row >= sp.first && row + 32 <= hi && h[0].there && h[1].there;
         float tm = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float x = fmaf(bf16_lo(kp[i]), s[i], bf16_hi(kp[i]) * q_sum);
-            if constexpr (NG == 2) x += row_ror_f32(x, 8);       // the other group of the row
-            s[i] = ldexpf(x, s_exp) * a.scale2;
+        for (int i = 0; i < V; ++i) s[i] = fmaf(bf16_lo(kp[i]), s[i], bf16_hi(kp[i]) * q_sum);
+        if constexpr (NG == 2) {                                 // the other group of the row
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[i] += PACK ? dpp_f32<kHalfMirror>(s[i]) : row_ror_f32(s[i], 8);
+        }
+        if (far) {
+            asm volatile("");                                    // a branch, not selects in every tile
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[i] = ldexpf(s[i], s_exp - s_near);
         }
         if (!whole) {
+            asm volatile("");
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = row + 16 * (i >> 2) + 4 * kq + (i & 3);
-                const bool on = r >= sp.first && r < hi && h[i >> 2].there;
+            for (int i = 0; i < V; ++i) {
+                const int u = PACK ? upper : i >> 2, r = row + 16 * u + 4 * kq + (i & 3);
+                const bool on = r >= sp.first && r < hi && (u ? h[1].there : h[0].there);
                 s[i] = on ? s[i] : -INFINITY;
                 vp[i] = on ? vp[i] : 0u;                         // whatever lies there: weight and value 0
             }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tm = fmaxf(tm, s[i]);
+        for (int i = 0; i < V; ++i) tm = fmaxf(tm, s[i]);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(more)::value) load_par(hn, a.c.k_par, kp);
         __builtin_amdgcn_sched_barrier(0);
-        const float mn = fmaxf(m, max_rows_f32(tm));
-        const float f = __builtin_amdgcn_exp2f(m - mn);
-        const bool moved = __ballot(mn != m) != 0ull;
-        m = mn;
-        float top = 0.0f, vs[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(s[i] - mn);
-            vs[i] = bf16_lo(vp[i]);
-            top = fmaxf(top, vs[i]);
-        }
-        if (moved) {
+        // the reference stays until a score passes it by more than 1, then steps 1 past that score:
+        // weights stay below 4 and the sums are rescaled a few times a chunk, not at every new maximum
+        if constexpr (PACK) tm = fmaxf(tm, row_ror_f32(tm, 8));
+        tm = max_rows_f32(tm) * s_mul;
+        if (__ballot(tm > m + 1.0f) != 0ull) {
+            const float mn = tm > m + 1.0f ? tm + 1.0f : m, f = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
             l *= f;
             z *= f;
+            flush();
 #pragma unroll
-            for (int j = 0; j < NV; ++j) acc[j] *= f;
+            for (int j = 0; j < NV; ++j) {
+                acc[j] *= f;
+                low[j] *= f;
+            }
+        }
+        float top = 0.0f, vs[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], s_mul, -m));
+            vs[i] = bf16_lo(vp[i]);
+            top = fmaxf(top, vs[i]);
         }
         // a scale past the limit: the power of two moves, with two bits to spare
         if (__ballot(top >= limit) != 0ull && __ballot(top > 0.0f) != 0ull) {
@@ -367,32 +418,45 @@ __global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
 #pragma unroll
             for (int o = 1; o < 16; o <<= 1) w = fmaxf(w, __shfl_xor(w, o));
             const int e = __builtin_amdgcn_frexp_expf(w) + 2;     // every scale below 2^(e - 2)
-            const int n = 15 - e;
-            if (limit > 0.0f)
+            const int n = 14 - e;
+            if (limit > 0.0f) {
+                flush();
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[j][i] = ldexpf(acc[j][i], n - v_exp);
+                    for (int i = 0; i < 4; ++i) {
+                        acc[j][i] = ldexpf(acc[j][i], n - v_exp);
+                        low[j][i] = ldexpf(low[j][i], n - v_exp);
+                    }
+            }
             v_exp = n;
             limit = ldexpf(1.0f, e);
         }
-        uint32_t ph[4], pl[4];
+        uint32_t ph[V / 2], pl[V / 2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < V / 2; ++i) {
             const float x = s[2 * i] * ldexpf(vs[2 * i], v_exp), y = s[2 * i + 1] * ldexpf(vs[2 * i + 1], v_exp);
-            const f16x2_t hx = {(_Float16)x, (_Float16)y};
-            const f16x2_t lx = {(_Float16)(x - (float)hx[0]), (_Float16)(y - (float)hx[1])};
+            const f16x2_t hx = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_pkrtz(rintf(x), rintf(y)));
+            const f32x2_t r = {fmaf(-1.0f, (float)hx[0], x), fmaf(-1.0f, (float)hx[1], y)};
             ph[i] = __builtin_bit_cast(uint32_t, hx);
-            pl[i] = __builtin_bit_cast(uint32_t, lx);
+            pl[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(r, f16x2_t));
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z = fmaf(s[i], bf16_hi(vp[i]), z);
-        l += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+        for (int i = 0; i < V; ++i) {
+            z = fmaf(s[i], bf16_hi(vp[i]), z);
+            l += s[i];
+        }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(more)::value) load_par(hn, a.c.v_par, vp);
         __builtin_amdgcn_sched_barrier(0);
-        const f16x8_t bh = __builtin_bit_cast(f16x8_t, u32x4_t{ph[0], ph[1], ph[2], ph[3]});
-        const f16x8_t bl = __builtin_bit_cast(f16x8_t, u32x4_t{pl[0], pl[1], pl[2], pl[3]});
+        // positions 0 .. 3 of the operand are the lower half's, 4 .. 7 the upper half's
+        u32x4_t bh, bl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool mine = !PACK || (i >> 1) == upper;
+            bh[i] = mine ? ph[i % (V / 2)] : 0u;
+            bl[i] = mine ? pl[i % (V / 2)] : 0u;
+        }
 #pragma unroll
         for (int w = 0; w < NV / 4; ++w) {
             uint32_t r[4][4];                                    // [code][pair of positions]
@@ -408,13 +472,14 @@ __global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[j][0], r[j][1], r[j][2], r[j][3]});
-                acc[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, bh, acc[4 * w + j], 0, 0, 0);
-                acc[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, bl, acc[4 * w + j], 0, 0, 0);
+                low[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, __builtin_bit_cast(f16x8_t, bl), low[4 * w + j], 0, 0, 0);
+                run[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, __builtin_bit_cast(f16x8_t, bh), run[4 * w + j], 0, 0, 0);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(more)::value) load_v(hn);
         __builtin_amdgcn_sched_barrier(0);
+        if (it % kFlush == kFlush - 1) flush();
     };
     if (n_it > 0) {
         halves(0, h0);
@@ -429,23 +494,35 @@ __global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
             h0[1] = h1[1];
         }
         tile(n_it - 1, h0, h0, std::false_type{});
+        flush();
+    }
+    if constexpr (PACK) {
+        l += row_ror_f32(l, 8);
+        z += row_ror_f32(z, 8);
     }
     l = add16_f32(l, l);
     l = add32_f32(l, l);
     z = add16_f32(z, z);
     z = add32_f32(z, z);
-    if (lane < 8) {
-        s_m[wave][lane] = m;
-        s_l[wave][lane] = l;
+    if (lane < 8 && gr == 0) {
+        s_m[wave][hc] = m;
+        s_l[wave][hc] = l;
     }
     // rows 4 kq + i of product j are elements (4 kq + i) * (D / 16) + j, right in the columns of
     // their own group
-    if (col < 8 * NG && (NG == 1 || (kq >> 1) == gr)) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float o = ldexpf(acc[j][i] + low[j][i], kCodeExp - v_exp);
+            if constexpr (PACK) o += row_ror_f32(o, 8);
+            acc[j][i] = o + z;
+        }
+    if (!(PACK && col >= 8) && (NG == 1 || (kq >> 1) == gr)) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                s_o[wave][col & 7][(4 * kq + i) * (D / 16) + j] = ldexpf(acc[j][i], kCodeExp - v_exp) + z;
+            for (int i = 0; i < 4; ++i) s_o[wave][hc][(4 * kq + i) * (D / 16) + j] = acc[j][i];
     }
     __syncthreads();
     for (int i = tid; i < a.group * D; i += kAttendThreads) {
@@ -463,39 +540,66 @@ __global__ __launch_bounds__(kAttendThreads, 3) void k_attend4(AttendArgs a)
     }
 }
 
-// Joins a token's chunks: block = (token, query head).
+// Joins a token's chunks: block = (token, query head), whose waves fold kMergeUnroll chunks at
+// a time, all of them read in one round trip, and are then joined themselves.
+constexpr int kMergeWaves = 16, kMergeUnroll = 8;
 template <int D>
-__global__ __launch_bounds__(kAttendThreads) void k_attend_merge(AttendArgs a)
+__global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
 {
-    constexpr int P = kAttendThreads / D, NW = kAttendThreads / 64;
-    __shared__ float s_red[NW], s_o[P][D], s_l[P];
+    constexpr int E = D / 64, U = kMergeUnroll;
+    __shared__ float s_o[kMergeWaves][D];
+    __shared__ float2 s_ml[kMergeWaves];
     const int64_t row = blockIdx.x, t = row / a.n_q;
     const Span sp = span_of(a, a.seq[t], a.pos[t]);
     const int nch = (sp.len - sp.base + a.chunk_rows - 1) / a.chunk_rows;
-    const int tid = threadIdx.x, e = tid % D, part = tid / D;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
     const float2 *ml = a.part_ml + row * a.chunks;
-    float m = -FLT_MAX;
-    for (int c = tid; c < nch; c += kAttendThreads) m = fmaxf(m, ml[c].x);
-    m = block_reduce<kAttendThreads>(m, s_red, [](float x, float y) { return fmaxf(x, y); });
-    float o = 0.0f, l = 0.0f;
-    for (int c = part; c < nch; c += P) {
-        const float2 x = ml[c];
-        const float f = exp2f(x.x - m);
-        l = fmaf(f, x.y, l);
-        o = fmaf(f, a.part_o[(row * a.chunks + c) * D + e], o);
-    }
-    s_o[part][e] = o;
-    if (e == 0) s_l[part] = l;
-    __syncthreads();
-    if (part == 0) {
+    const float *po = a.part_o + row * a.chunks * D + lane * E;
+    float m = -FLT_MAX, l = 0.0f, o[E] = {};
+    for (int c0 = wave * U; c0 < nch; c0 += waves * U) {
+        float2 x[U];
+        float v[U][E];
 #pragma unroll
-        for (int p = 1; p < P; ++p) {
-            o += s_o[p][e];
-            l += s_l[p];
+        for (int u = 0; u < U; ++u) {
+            const int c = min(c0 + u, nch - 1);
+            x[u] = ml[c];
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[u][e] = po[(int64_t)c * D + e];
         }
-        a.out[row * D + e] = l > 0.0f ? o / l : 0.0f;
-        if (e == 0 && a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+        float mn = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) mn = fmaxf(mn, x[u].x);
+        const float f = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float w = c0 + u < nch ? __builtin_amdgcn_exp2f(x[u].x - mn) : 0.0f;
+            l = fmaf(w, x[u].y, l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(w, v[u][e], o[e]);
+        }
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_o[wave][lane * E + e] = o[e];
+    if (lane == 0) s_ml[wave] = make_float2(m, l);
+    __syncthreads();
+    if (tid >= 64) return;
+    for (int w = 0; w < waves; ++w) m = fmaxf(m, s_ml[w].x);
+    l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.0f;
+    for (int w = 0; w < waves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_ml[w].x - m);
+        l = fmaf(f, s_ml[w].y, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(f, s_o[w][lane * E + e], o[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) a.out[row * D + lane * E + e] = l > 0.0f ? o[e] / l : 0.0f;
+    if (lane == 0 && a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 template <typename T, int D, int FMT> const void *attend_kernel(int group)
@@ -503,11 +607,16 @@ template <typename T, int D, int FMT> const void *attend_kernel(int group)
     return group <= 1 ? (const void *)&k_attend<T, D, 1, FMT> : group <= 2 ? (const void *)&k_attend<T, D, 2, FMT>
            : group <= 4 ? (const void *)&k_attend<T, D, 4, FMT> : (const void *)&k_attend<T, D, 8, FMT>;
 }
+template <typename T> const void *attend4_kernel(int d, int group)
+{
+    if (d == 64) return (const void *)&k_attend4<T, 64, true>;
+    return group <= 4 ? (const void *)&k_attend4<T, 128, true> : (const void *)&k_attend4<T, 128, false>;
+}
 template <int D> const void *attend_kernel(int format, int dtype, int group)
 {
     if (format == RETOPK_PAGES_BF16) return attend_kernel<uint16_t, D, RETOPK_PAGES_BF16>(group);
     if (format == RETOPK_PAGES_F32) return attend_kernel<float, D, RETOPK_PAGES_F32>(group);
-    return dtype == RETOPK_BF16 ? (const void *)&k_attend4<uint16_t, D> : (const void *)&k_attend4<float, D>;
+    return dtype == RETOPK_BF16 ? attend4_kernel<uint16_t>(D, group) : attend4_kernel<float>(D, group);
 }
 
 // Checks the arguments the workspace depends on and makes the plan.
@@ -585,7 +694,9 @@ retopk_status paged_attention(const retopk_pages *c, int32_t dtype, int64_t n_to
         return RETOPK_ERR_HIP;
     if (p.chunks > 1) {
         f = d == 64 ? (const void *)&k_attend_merge<64> : (const void *)&k_attend_merge<128>;
-        if (hipLaunchKernel(f, dim3((unsigned)(n_tokens * n_q_heads)), dim3(kAttendThreads), args, 0, s) != hipSuccess)
+        // a wave for kMergeUnroll chunks
+        const int64_t need = ceil_div(p.chunks, kMergeUnroll), waves = need < kMergeWaves ? need : kMergeWaves;
+        if (hipLaunchKernel(f, dim3((unsigned)(n_tokens * n_q_heads)), dim3((unsigned)(64 * waves)), args, 0, s) != hipSuccess)
             return RETOPK_ERR_HIP;
     }
     return RETOPK_OK;
