@@ -11,7 +11,11 @@
 namespace retopk {
 namespace {
 
-constexpr int kAttendThreads = 256;
+constexpr int kAttendThreads = 64 * kAttendWaves;
+#ifndef AB
+#define AB 2048
+#endif
+constexpr int kAttendSlots = AB;    // two waves a SIMD
 constexpr float kLn2 = 0.69314718055994530942f;
 
 struct AttendArgs {
@@ -19,19 +23,21 @@ struct AttendArgs {
     const int32_t *seq, *pos;
     const char *q;             // element strides
     int64_t q_ts, q_hs;
-    int32_t n_q, group;        // query heads; of a KV head
+    int32_t n_tokens, n_q, group;      // query heads; of a KV head
     int32_t max_len, window;
-    int32_t chunk_rows, chunks;
+    int32_t split, waves, chunks;      // AttendPlan
     float scale2;              // log2(e) / sqrt(d): scores are in powers of two
-    float *out, *lse;          // chunks == 1
-    float *part_o;             // else [tokens * n_q, chunks, d]
-    float2 *part_ml;           // [tokens * n_q, chunks]: maximum (a power of two), sum
+    float *out, *lse;
+    int32_t *ends;             // BALANCED: [n_tokens] tiles up to and with a token, then a part's tiles
+    float *part_o;             // [parts, group, d]
+    float2 *part_ml;           // [parts, group]: maximum (a power of two), sum
 };
 
-// The attended positions [first, len) of a token, len = 0 where there are none; chunk c
-// begins at first rounded down to a tile, + c * chunk_rows.
+// The attended positions [first, len) of a token, len = 0 where there are none; its tiles
+// begin at base.
 struct Span {
     int first, len, base;
+    __device__ __forceinline__ int tiles() const { return (len - base + kAttendTile - 1) / kAttendTile; }
 };
 __device__ __forceinline__ Span span_of(const AttendArgs &a, int32_t s, int32_t p)
 {
@@ -44,17 +50,96 @@ __device__ __forceinline__ Span span_of(const AttendArgs &a, int32_t s, int32_t 
     return r;
 }
 
-// Writes the result of a token's head, or of one of its chunks.
-__device__ __forceinline__ void write_result(const AttendArgs &a, int64_t row, int chunk, int d, int e, float o,
-                                             float m, float l)
-{
-    if (a.chunks == 1) {
-        a.out[row * d + e] = l > 0.0f ? o / l : 0.0f;
-        if (e == 0 && a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
-    } else {
-        a.part_o[(row * a.chunks + chunk) * d + e] = o;
-        if (e == 0) a.part_ml[row * a.chunks + chunk] = make_float2(m, l);
+// One wave's share of a group: positions [lo, hi) of token t for KV head g, within the token's
+// span; the result goes to the output (part < 0) or to that partial result.
+struct Share {
+    int64_t t;
+    int g, seq, lo, hi;
+    Span span;
+    int64_t part;
+    // row of head j of the group in the output or among the partial results
+    __device__ __forceinline__ int64_t row(const AttendArgs &a, int j) const
+    {
+        return part < 0 ? t * a.n_q + g * a.group + j : part * a.group + j;
     }
+};
+
+// Runs f on every share of this wave.
+template <typename F>
+__device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
+{
+    __shared__ int s_ends[kAttendTokens], s_seq[kAttendTokens], s_pos[kAttendTokens];
+    __shared__ uint32_t s_red[kAttendWaves];
+    static_assert(kAttendTokens == kAttendThreads, "a token a thread");
+    const int hkv = a.c.n_kv_heads, tid = threadIdx.x, lane = tid & 63;
+    const int worker = blockIdx.x * kAttendWaves + __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool balanced = a.split == ATTEND_BALANCED;
+    int at = 0, last = worker < a.waves ? 1 : 0;
+    if (balanced) {
+        // every token's last tile (of all KV heads), counted by each block for itself
+        const int sq = tid < a.n_tokens ? a.seq[tid] : -1, p = tid < a.n_tokens ? a.pos[tid] : -1;
+        const int n = span_of(a, sq, p).tiles() * hkv;
+        uint32_t all;
+        const int end = (int)block_excl_scan<kAttendThreads>((uint32_t)n, s_red, &all) + n;
+        const int per = (int)attend_part(all, (uint32_t)a.waves);
+        s_ends[tid] = end;
+        s_seq[tid] = sq;
+        s_pos[tid] = p;
+        if (blockIdx.x == 0 && tid < a.n_tokens) {
+            a.ends[tid] = end;
+            if (tid == 0) a.ends[a.n_tokens] = per;
+        }
+        __syncthreads();
+        const int64_t from = (int64_t)worker * per;
+        at = (int)min(from, (int64_t)all);
+        last = (int)min(from + per, (int64_t)all);
+    }
+    while (at < last) {
+        Share w;
+        int step = 1;
+        if (balanced) {
+            // the token that holds tile `at`: as many as end at or before it come first
+            int t = 0;
+            for (int i = 0; i < a.n_tokens; i += 64)
+                t += __popcll(__ballot(i + lane < a.n_tokens && s_ends[i + lane] <= at));
+            t = __builtin_amdgcn_readfirstlane(t);
+            const int start = t > 0 ? __builtin_amdgcn_readfirstlane(s_ends[t - 1]) : 0;
+            const int tiles = (__builtin_amdgcn_readfirstlane(s_ends[t]) - start) / hkv;
+            const int first = (at - start) % tiles;
+            step = min(tiles - first, last - at);
+            w.t = t;
+            w.g = (at - start) / tiles;
+            w.seq = __builtin_amdgcn_readfirstlane(s_seq[t]);
+            w.span = span_of(a, w.seq, __builtin_amdgcn_readfirstlane(s_pos[t]));
+            w.lo = w.span.base + first * kAttendTile;
+            w.hi = min(w.span.len, w.lo + step * kAttendTile);
+            w.part = step == tiles ? -1 : (int64_t)worker + (int64_t)t * hkv + w.g;
+        } else {
+            const int chunk = worker % a.chunks, bg = worker / a.chunks;
+            w.t = bg / hkv;
+            w.g = bg % hkv;
+            w.seq = __builtin_amdgcn_readfirstlane(a.seq[w.t]);
+            w.span = span_of(a, w.seq, __builtin_amdgcn_readfirstlane(a.pos[w.t]));
+            w.lo = w.span.base + chunk * kAttendChunk;
+            w.hi = min(w.span.len, w.lo + kAttendChunk);
+            w.part = a.split == ATTEND_DIRECT ? -1 : (int64_t)worker;
+            if (a.split == ATTEND_DIRECT) w.hi = w.span.len;
+        }
+        if (w.lo < w.hi || w.part < 0) f(w);
+        at += step;
+    }
+}
+
+// The weights' sum l and reference m of head j of a share; what its value sums are times.
+__device__ __forceinline__ void write_sum(const AttendArgs &a, const Share &w, int j, float m, float l)
+{
+    const int64_t row = w.row(a, j);
+    if (w.part >= 0) a.part_ml[row] = make_float2(m, l);
+    else if (a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+__device__ __forceinline__ float out_factor(const Share &w, float l)
+{
+    return w.part >= 0 ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
 }
 
 // The plain kernel: D / 8 lanes a row, every position's scores, maximum and weights in
@@ -62,92 +147,66 @@ __device__ __forceinline__ void write_result(const AttendArgs &a, int64_t row, i
 template <typename T, int D, int GP, int FMT>
 __global__ __launch_bounds__(kAttendThreads) void k_attend(AttendArgs a)
 {
-    constexpr int LPR = D / 8, SLOTS = kAttendThreads / LPR, NW = kAttendThreads / 64;
-    __shared__ float s_m[NW][GP], s_l[NW][GP], s_o[NW][GP][D];
-    const int chunk = blockIdx.x % a.chunks, bg = blockIdx.x / a.chunks;
-    const int g = bg % a.c.n_kv_heads;
-    const int64_t t = bg / a.c.n_kv_heads;
-    const int32_t sq = a.seq[t];
-    const Span sp = span_of(a, sq, a.pos[t]);
-    const int lo = sp.base + chunk * a.chunk_rows, hi = min(sp.len, lo + a.chunk_rows);
-    if (lo >= hi && !(chunk == 0 && a.chunks == 1)) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e0 = tid % LPR * 8;
-
-    float q[GP][8], acc[GP][8], m[GP], l[GP];
+    constexpr int LPR = D / 8, SLOTS = 64 / LPR;
+    for_shares(a, [&](const Share &w) {
+        const int lane = threadIdx.x & 63, e0 = lane % LPR * 8;
+        float q[GP][8], acc[GP][8], m[GP], l[GP];
 #pragma unroll
-    for (int j = 0; j < GP; ++j) {
-        const int h = g * a.group + (j < a.group ? j : 0);
-        Oct<T> v;
-        v.load((const T *)a.q + t * a.q_ts + h * a.q_hs + e0);
-        v.get(q[j]);
-        m[j] = -FLT_MAX;
-        l[j] = 0.0f;
+        for (int j = 0; j < GP; ++j) {
+            const int h = w.g * a.group + (j < a.group ? j : 0);
+            Oct<T> v;
+            v.load((const T *)a.q + w.t * a.q_ts + h * a.q_hs + e0);
+            v.get(q[j]);
+            m[j] = -FLT_MAX;
+            l[j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[j][i] = 0.0f;
-    }
-    for (int r = max(lo, sp.first) + tid / LPR; r < hi; r += SLOTS) {
-        const int64_t row = row_of(a.c, sq, r, g);
-        if (row < 0) continue;
-        float k[8], v[8];
-        if constexpr (FMT == RETOPK_PAGES_Q4) {
-            const int64_t w = row * (D / 8) + e0 / 8, par = row * (D / kGroup4) + e0 / kGroup4;
-            values4(((const uint32_t *)a.c.k)[w], a.c.k_par[par], k);
-            values4(((const uint32_t *)a.c.v)[w], a.c.v_par[par], v);
-        } else {
+            for (int i = 0; i < 8; ++i) acc[j][i] = 0.0f;
+        }
+        for (int r = max(w.lo, w.span.first) + lane / LPR; r < w.hi; r += SLOTS) {
+            const int64_t row = row_of(a.c, w.seq, r, w.g);
+            if (row < 0) continue;
+            float k[8], v[8];
             Oct<T> x, y;
             x.load((const T *)a.c.k + row * D + e0);
             y.load((const T *)a.c.v + row * D + e0);
             x.get(k);
             y.get(v);
+#pragma unroll
+            for (int j = 0; j < GP; ++j) {
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s = fmaf(q[j][i], k[i], s);
+#pragma unroll
+                for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
+                s *= a.scale2;
+                const float mn = fmaxf(m[j], s), f = exp2f(m[j] - mn), p = exp2f(s - mn);
+                m[j] = mn;
+                l[j] = l[j] * f + p;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[j][i] = fmaf(p, v[i], acc[j][i] * f);
+            }
         }
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
-            float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(q[j][i], k[i], s);
+            for (int o = LPR; o < 64; o <<= 1) {
+                const float m2 = __shfl_xor(m[j], o), l2 = __shfl_xor(l[j], o), mn = fmaxf(m[j], m2);
+                const float f = exp2f(m[j] - mn), f2 = exp2f(m2 - mn);
+                m[j] = mn;
+                l[j] = l[j] * f + l2 * f2;
 #pragma unroll
-            for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
-            s *= a.scale2;
-            const float mn = fmaxf(m[j], s), f = exp2f(m[j] - mn), p = exp2f(s - mn);
-            m[j] = mn;
-            l[j] = l[j] * f + p;
+                for (int i = 0; i < 8; ++i) acc[j][i] = acc[j][i] * f + __shfl_xor(acc[j][i], o) * f2;
+            }
+            if (lane < LPR && j < a.group) {
+                const float f = out_factor(w, l[j]);
+                float *o = (w.part < 0 ? a.out : a.part_o) + w.row(a, j) * D + e0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[j][i] = fmaf(p, v[i], acc[j][i] * f);
+                for (int i = 0; i < 8; ++i) acc[j][i] *= f;
+                Oct<float>::store(o, acc[j]);
+                if (lane == 0) write_sum(a, w, j, m[j], l[j]);
+            }
         }
-    }
-    // the wave's slots, then the waves
-#pragma unroll
-    for (int j = 0; j < GP; ++j) {
-#pragma unroll
-        for (int o = LPR; o < 64; o <<= 1) {
-            const float m2 = __shfl_xor(m[j], o), l2 = __shfl_xor(l[j], o), mn = fmaxf(m[j], m2);
-            const float f = exp2f(m[j] - mn), f2 = exp2f(m2 - mn);
-            m[j] = mn;
-            l[j] = l[j] * f + l2 * f2;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[j][i] = acc[j][i] * f + __shfl_xor(acc[j][i], o) * f2;
-        }
-        if (lane < LPR) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s_o[wave][j][e0 + i] = acc[j][i];
-            s_m[wave][j] = m[j];
-            s_l[wave][j] = l[j];
-        }
-    }
-    __syncthreads();
-    for (int i = tid; i < a.group * D; i += kAttendThreads) {
-        const int j = i / D, e = i % D;
-        float mx = s_m[0][j], o = 0.0f, ls = 0.0f;
-#pragma unroll
-        for (int w = 1; w < NW; ++w) mx = fmaxf(mx, s_m[w][j]);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float f = exp2f(s_m[w][j] - mx);
-            o += f * s_o[w][j][e];
-            ls += f * s_l[w][j];
-        }
-        write_result(a, t * a.n_q + g * a.group + j, chunk, D, e, o, mx, ls);
-    }
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -163,21 +222,20 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 // float16 c * 2^-20, exact; code 1 lies four bits lower, codes 2 and 3 the same with the
 // bytes swapped.  One and-or a pair of codes, no conversion.
 constexpr int kCodeExp = 20;
-__device__ __forceinline__ uint32_t code_pair(uint32_t x)
-{
-    // (x & 0x80708070) | 0x00080008; the compiler makes two instructions of it
-    uint32_t r;
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(0x80708070u), "v"(0x00080008u));
-    return r;
-}
-__device__ __forceinline__ void code_quad(uint32_t x, uint32_t (&r)[4])
-{
-    const uint32_t y = __builtin_amdgcn_perm(x, x, 0x02030001u);
-    r[0] = code_pair(x);
-    r[1] = code_pair(x << 4);
-    r[2] = code_pair(y);
-    r[3] = code_pair(y << 4);
-}
+struct Codes {
+    uint32_t mask = 0x80708070u, half = 0x00080008u;
+    // held in registers, so that (x & mask) | half is one instruction (literals would make it two)
+    __device__ __forceinline__ void hold() { asm volatile("" : "+s"(mask), "+v"(half)); }
+    __device__ __forceinline__ uint32_t pair(uint32_t x) const { return (x & mask) | half; }
+    __device__ __forceinline__ void quad(uint32_t x, uint32_t (&r)[4]) const
+    {
+        const uint32_t y = __builtin_amdgcn_perm(x, x, 0x02030001u);
+        r[0] = pair(x);
+        r[1] = pair(x << 4);
+        r[2] = pair(y);
+        r[3] = pair(y << 4);
+    }
+};
 
 // Base rows of the two 16-position halves of a tile: a 4-bit page holds whole halves, so
 // that a half has one page, looked up once for the wave.
@@ -212,29 +270,24 @@ constexpr int kFlush = 4;
 template <typename T, int D, bool PACK>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
 {
-    constexpr int NW = kAttendThreads / 64, NG = D / kGroup4;
+    constexpr int NG = D / kGroup4;
     constexpr int V = PACK ? 4 : 8;            // positions a lane weighs in a tile
     constexpr int KD = D / 32;                 // code dwords of a lane's share of a key row
     constexpr int NV = D / 16;                 // value products: codes of a lane's share of a row
     constexpr int NQ = sizeof(T) == 4 ? 2 : 1; // float16 parts of the query
     static_assert(PACK || NG == 2, "d = 64 always packs");
-    __shared__ float s_m[NW][8], s_l[NW][8], s_o[NW][8][D];
-    const int chunk = blockIdx.x % a.chunks, bg = blockIdx.x / a.chunks;
-    const int g = bg % a.c.n_kv_heads;
-    const int64_t t = bg / a.c.n_kv_heads;
-    const int32_t sq = a.seq[t];
-    const Span sp = span_of(a, sq, a.pos[t]);
-    const int lo = sp.base + chunk * a.chunk_rows, hi = min(sp.len, lo + a.chunk_rows);
-    if (lo >= hi && !(chunk == 0 && a.chunks == 1)) return;
-    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for_shares(a, [&](const Share &w) {
+    const int g = w.g, lo = w.lo, hi = w.hi;
+    const int lane = threadIdx.x & 63, col = lane & 15, kq = lane >> 4;
+    Codes codes;
+    codes.hold();
     // group and head of this lane's column; packed columns 4 .. 7 of d = 128 count the heads down,
     // so that a half-row mirror meets the other group of the same head
     const int c8 = col & 7, upper = PACK ? col >> 3 : 0;
     const int gr = NG == 1 ? 0 : PACK ? c8 >> 2 : col >> 3;
     const int hc = PACK && NG == 2 ? (gr ? 7 - c8 : c8) : c8, head = hc < a.group ? hc : 0;
-    const int n_it = (hi - lo + 32 * NW - 1 - 32 * wave) / (32 * NW);
-    const int32_t *table = a.c.table + (int64_t)(sq < 0 ? 0 : sq) * a.c.table_width;
+    const int n_it = (hi - lo + 31) / 32;
+    const int32_t *table = a.c.table + (int64_t)max(w.seq, 0) * a.c.table_width;
 
     // the query, scaled by a power of two to [2^14, 2^15): bf16 fits one float16 part, f32 two
     f16x8_t qb[NQ][KD];
@@ -242,7 +295,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
     float q_sum = 0.0f;
     {
         float x[KD][8], top = 0.0f;
-        const T *qr = (const T *)a.q + t * a.q_ts + (g * a.group + head) * a.q_hs + kq * (D / 4);
+        const T *qr = (const T *)a.q + w.t * a.q_ts + (g * a.group + head) * a.q_hs + kq * (D / 4);
 #pragma unroll
         for (int i = 0; i < KD; ++i) {
             Oct<T> v;
@@ -278,7 +331,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
     uint32_t kp[V], vp[V], vc[8];
     Half h0[2], h1[2];         // this tile's halves, the next one's
     auto halves = [&](int it, Half (&h)[2]) {
-        const int r = lo + (it * NW + wave) * 32;
+        const int r = lo + it * 32;
 #pragma unroll
         for (int u = 0; u < 2; ++u) h[u] = half_of(a.c, table, r + 16 * u, g);
     };
@@ -348,7 +401,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
 #pragma unroll
                 for (int i = 0; i < KD; ++i) {
                     uint32_t r[4];
-                    code_quad(kc[u][i], r);
+                    codes.quad(kc[u][i], r);
                     const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[0], r[1], r[2], r[3]});
 #pragma unroll
                     for (int n = NQ - 1; n >= 0; --n) d[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qb[n][i], d[u], 0, 0, 0);
@@ -360,8 +413,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(more)::value) load_k(hn);
         __builtin_amdgcn_sched_barrier(0);
-        const int row = lo + (it * NW + wave) * 32;
-        const bool whole = row >= sp.first && row + 32 <= hi && h[0].there && h[1].there;
+        const int row = lo + it * 32;
+        const bool whole = row >= w.span.first && row + 32 <= hi && h[0].there && h[1].there;
         float tm = -INFINITY;
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = fmaf(bf16_lo(kp[i]), s[i], bf16_hi(kp[i]) * q_sum);
@@ -379,7 +432,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int u = PACK ? upper : i >> 2, r = row + 16 * u + 4 * kq + (i & 3);
-                const bool on = r >= sp.first && r < hi && (u ? h[1].there : h[0].there);
+                const bool on = r >= w.span.first && r < hi && (u ? h[1].there : h[0].there);
                 s[i] = on ? s[i] : -INFINITY;
                 vp[i] = on ? vp[i] : 0u;                         // whatever lies there: weight and value 0
             }
@@ -464,10 +517,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
             for (int i = 0; i < 4; ++i) {
                 const uint32_t x = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], w ? 0x07060302u : 0x05040100u);
                 const uint32_t y = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], w ? 0x06070203u : 0x04050001u);
-                r[0][i] = code_pair(x);
-                r[1][i] = code_pair(x << 4);
-                r[2][i] = code_pair(y);
-                r[3][i] = code_pair(y << 4);
+                r[0][i] = codes.pair(x);
+                r[1][i] = codes.pair(x << 4);
+                r[2][i] = codes.pair(y);
+                r[3][i] = codes.pair(y << 4);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -504,45 +557,31 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
     l = add32_f32(l, l);
     z = add16_f32(z, z);
     z = add32_f32(z, z);
-    if (lane < 8 && gr == 0) {
-        s_m[wave][hc] = m;
-        s_l[wave][hc] = l;
-    }
+    if (lane < 8 && gr == 0 && hc < a.group) write_sum(a, w, hc, m, l);
     // rows 4 kq + i of product j are elements (4 kq + i) * (D / 16) + j, right in the columns of
     // their own group
+    const float f = out_factor(w, l);
+    float *out = (w.part < 0 ? a.out : a.part_o) + w.row(a, hc) * D + 4 * kq * (D / 16);
+    const bool mine = !(PACK && col >= 8) && (NG == 1 || (kq >> 1) == gr) && hc < a.group;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float o = ldexpf(acc[j][i] + low[j][i], kCodeExp - v_exp);
-            if constexpr (PACK) o += row_ror_f32(o, 8);
-            acc[j][i] = o + z;
+        for (int j0 = 0; j0 < NV; j0 += 4) {
+            f32x4_t o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                o[j] = ldexpf(acc[j0 + j][i] + low[j0 + j][i], kCodeExp - v_exp);
+                if constexpr (PACK) o[j] += row_ror_f32(o[j], 8);
+                o[j] = (o[j] + z) * f;
+            }
+            if (mine) *(f32x4_t *)(out + i * (D / 16) + j0) = o;
         }
-    if (!(PACK && col >= 8) && (NG == 1 || (kq >> 1) == gr)) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s_o[wave][hc][(4 * kq + i) * (D / 16) + j] = acc[j][i];
-    }
-    __syncthreads();
-    for (int i = tid; i < a.group * D; i += kAttendThreads) {
-        const int j = i / D, e = i % D;
-        float mx = s_m[0][j], o = 0.0f, ls = 0.0f;
-#pragma unroll
-        for (int w = 1; w < NW; ++w) mx = fmaxf(mx, s_m[w][j]);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float f = __builtin_amdgcn_exp2f(s_m[w][j] - mx);
-            o += f * s_o[w][j][e];
-            ls += f * s_l[w][j];
-        }
-        write_result(a, t * a.n_q + g * a.group + j, chunk, D, e, o, mx, ls);
-    }
+    });
 }
 
-// Joins a token's chunks: block = (token, query head), whose waves fold kMergeUnroll chunks at
+// Joins the parts of a group: block = (token, query head), whose waves fold kMergeUnroll parts at
 // a time, all of them read in one round trip, and are then joined themselves.
-constexpr int kMergeWaves = 16, kMergeUnroll = 8;
+constexpr int kMergeWaves = 16, kMergeUnroll = 16;
 template <int D>
 __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
 {
@@ -550,11 +589,24 @@ __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
     __shared__ float s_o[kMergeWaves][D];
     __shared__ float2 s_ml[kMergeWaves];
     const int64_t row = blockIdx.x, t = row / a.n_q;
-    const Span sp = span_of(a, a.seq[t], a.pos[t]);
-    const int nch = (sp.len - sp.base + a.chunk_rows - 1) / a.chunk_rows;
+    const int h = (int)(row % a.n_q), g = h / a.group;
+    int64_t part;
+    int nch;
+    if (a.split == ATTEND_BALANCED) {
+        const int per = a.ends[a.n_tokens], start = t > 0 ? a.ends[t - 1] : 0;
+        const int tiles = (a.ends[t] - start) / a.c.n_kv_heads, from = start + g * tiles;
+        const int b0 = from / per, b1 = tiles > 0 ? (from + tiles - 1) / per : b0 - 1;
+        if (b0 == b1) return;      // all in one block, which wrote the output
+        nch = b1 - b0 + 1;
+        part = b0 + t * a.c.n_kv_heads + g;
+    } else {
+        nch = (span_of(a, a.seq[t], a.pos[t]).tiles() + kAttendChunk / kAttendTile - 1) / (kAttendChunk / kAttendTile);
+        part = (t * a.c.n_kv_heads + g) * a.chunks;
+    }
+    part = part * a.group + (h - g * a.group);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
-    const float2 *ml = a.part_ml + row * a.chunks;
-    const float *po = a.part_o + row * a.chunks * D + lane * E;
+    const float2 *ml = a.part_ml + part;
+    const float *po = a.part_o + part * D + lane * E;
     float m = -FLT_MAX, l = 0.0f, o[E] = {};
     for (int c0 = wave * U; c0 < nch; c0 += waves * U) {
         float2 x[U];
@@ -562,9 +614,9 @@ __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = min(c0 + u, nch - 1);
-            x[u] = ml[c];
+            x[u] = ml[(int64_t)c * a.group];
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[u][e] = po[(int64_t)c * D + e];
+            for (int e = 0; e < E; ++e) v[u][e] = po[(int64_t)c * a.group * D + e];
         }
         float mn = m;
 #pragma unroll
@@ -630,8 +682,8 @@ retopk_status plan_of(const retopk_pages &c, int64_t n_tokens, int32_t n_q_heads
     if (n_tokens >= limit || n_tokens * n_q_heads >= limit) return RETOPK_ERR_UNSUPPORTED;
     if (max_len > rows) max_len = rows;
     if (window > rows) window = 0;
-    *out = attend_plan(n_tokens, n_q_heads, c.n_kv_heads, c.head_dim, max_len, window);
-    return out->blocks < limit ? RETOPK_OK : RETOPK_ERR_UNSUPPORTED;
+    *out = attend_plan(n_tokens, n_q_heads, c.n_kv_heads, c.head_dim, max_len, window, kAttendSlots);
+    return out->waves < limit ? RETOPK_OK : RETOPK_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -670,6 +722,9 @@ retopk_status paged_attention(const retopk_pages *c, int32_t dtype, int64_t n_to
     }
     const int64_t rows = (int64_t)c->page_size * c->table_width;
     AttendArgs a = {};
+    a.n_tokens = (int32_t)n_tokens;
+    a.split = p.split;
+    a.waves = (int32_t)p.waves;
     a.c = pages_args(*c);
     a.seq = seq;
     a.pos = pos;
@@ -680,22 +735,23 @@ retopk_status paged_attention(const retopk_pages *c, int32_t dtype, int64_t n_to
     a.group = n_q_heads / c->n_kv_heads;
     a.max_len = (int32_t)(max_len < rows ? max_len : rows);
     a.window = window <= rows ? (int32_t)window : 0;
-    a.chunk_rows = (int32_t)p.chunk_rows;
     a.chunks = (int32_t)p.chunks;
     a.scale2 = (float)(1.44269504088896340736 / __builtin_sqrt((double)d));
     a.out = out;
     a.lse = lse;
-    a.part_o = (float *)workspace;
-    a.part_ml = (float2 *)((float *)workspace + n_tokens * n_q_heads * p.chunks * d);
+    a.ends = (int32_t *)workspace;
+    a.part_o = (float *)((char *)workspace + p.ends_bytes);
+    a.part_ml = (float2 *)(a.part_o + p.parts * a.group * d);
     hipStream_t s = (hipStream_t)stream;
     void *args[1] = {&a};
     const void *f = d == 64 ? attend_kernel<64>(c->format, dtype, a.group) : attend_kernel<128>(c->format, dtype, a.group);
-    if (hipLaunchKernel(f, dim3((unsigned)p.blocks), dim3(kAttendThreads), args, 0, s) != hipSuccess)
+    if (hipLaunchKernel(f, dim3((unsigned)ceil_div(p.waves, kAttendWaves)), dim3(kAttendThreads), args, 0, s) != hipSuccess)
         return RETOPK_ERR_HIP;
-    if (p.chunks > 1) {
+    if (p.split != ATTEND_DIRECT) {
         f = d == 64 ? (const void *)&k_attend_merge<64> : (const void *)&k_attend_merge<128>;
-        // a wave for kMergeUnroll chunks
-        const int64_t need = ceil_div(p.chunks, kMergeUnroll), waves = need < kMergeWaves ? need : kMergeWaves;
+        // waves for the parts of a group four times as long as the mean, at most
+        const int64_t parts = ceil_div(4 * p.parts, n_tokens * c->n_kv_heads), need = ceil_div(parts, kMergeUnroll);
+        const int64_t waves = need < kMergeWaves ? need : kMergeWaves;
         if (hipLaunchKernel(f, dim3((unsigned)(n_tokens * n_q_heads)), dim3((unsigned)(64 * waves)), args, 0, s) != hipSuccess)
             return RETOPK_ERR_HIP;
     }

@@ -28,37 +28,67 @@ constexpr uint32_t divide(uint32_t x, Divisor d)
     return (uint32_t)(((uint64_t)x * d.magic) >> (31 + d.shift));
 }
 
-// paged_attention: block (chunk, KV head, token) takes chunk_rows positions of one token's
-// sequence, counted from its first attended position rounded down to a tile.  The lengths
-// are on the device, so the grid is sized for max_len and blocks past a sequence's end
-// leave at once.
-constexpr int kAttendTile = 32;       // positions of a wave's tile
-constexpr int kAttendBlocks = 1024;   // blocks that fill the chip
-constexpr int kAttendRowsMin = 256;
-constexpr int kAttendRowsMax = 2048;
+// paged_attention: how the positions of all (token, KV head) groups are shared out over waves,
+// each of which works alone.  A token's positions count from its first attended one rounded
+// down to a tile.  The lengths are on the device, the host knows only max_len, so there are
+// three splits:
+//   DIRECT    one wave a group: no group has more than kAttendDirect tiles, and the wave
+//             writes the output itself.
+//   BALANCED  the tiles of all groups in one row, token after token, cut into equal parts on
+//             the device, one a wave, so that ragged lengths leave no wave idle; a part may
+//             span several groups and a group several parts.  At most kAttendTokens tokens,
+//             whose tile counts each block sums up for itself.
+//   CHUNKED   wave (token, KV head, chunk of kAttendChunk rows) for more tokens than that;
+//             waves past a sequence's end leave at once.
+// The partial results of BALANCED have numbers wave + group, which no two parts share (each
+// part of a wave begins a new group, each part of a group a new wave).
+constexpr int kAttendTile = 32;       // positions of a tile
+constexpr int kAttendDirect = 8;      // tiles
+constexpr int kAttendPart = 2;        // fewest tiles of a BALANCED wave
+constexpr int kAttendWaves = 4;       // of a block
+constexpr int kAttendTokens = 256;
+constexpr int kAttendChunk = 512;     // rows
 
+enum AttendSplit : int { ATTEND_DIRECT = 0, ATTEND_BALANCED = 1, ATTEND_CHUNKED = 2 };
 struct AttendPlan {
-    int64_t chunk_rows;        // a multiple of kAttendTile
-    int64_t chunks;            // chunks a token needs at most
-    int64_t blocks;            // of the whole grid
-    int64_t workspace;         // bytes of partial results; 0 with one chunk a token
+    int split;
+    int64_t waves;             // in blocks of kAttendWaves, of which the last may be part empty
+    int64_t chunks;            // CHUNKED: a group
+    int64_t parts;             // partial results of a KV head's query heads; 0: DIRECT
+    int64_t ends_bytes;        // BALANCED: the tile counts, at the workspace's start
+    int64_t workspace;         // bytes
 };
 
+// slots: the waves that run at once.
 inline AttendPlan attend_plan(int64_t tokens, int64_t n_q_heads, int64_t n_kv_heads, int d, int64_t max_len,
-                              int64_t window)
+                              int64_t window, int64_t slots)
 {
-    AttendPlan p;
+    AttendPlan p = {ATTEND_DIRECT, tokens * n_kv_heads, 1, 0, 0, 0};
     // a window's first position may lie kAttendTile - 1 past the tile it begins in
-    int64_t span = window > 0 && window + kAttendTile - 1 < max_len ? window + kAttendTile - 1 : max_len;
-    const int64_t groups = tokens * n_kv_heads;
-    int64_t rows = ceil_div(ceil_div(span * groups, kAttendBlocks), kAttendTile) * kAttendTile;
-    if (rows < kAttendRowsMin) rows = kAttendRowsMin;
-    if (rows > kAttendRowsMax) rows = kAttendRowsMax;
-    p.chunk_rows = rows;
-    p.chunks = ceil_div(span, rows);
-    p.blocks = groups * p.chunks;
-    p.workspace = p.chunks > 1 ? tokens * n_q_heads * p.chunks * (d + 2) * 4 : 0;
+    const int64_t span = window > 0 && window + kAttendTile - 1 < max_len ? window + kAttendTile - 1 : max_len;
+    const int64_t groups = tokens * n_kv_heads, tiles = ceil_div(span, kAttendTile);
+    if (tiles <= kAttendDirect) return p;
+    if (tokens <= kAttendTokens && groups * tiles < ((int64_t)1 << 31)) {
+        p.split = ATTEND_BALANCED;
+        const int64_t most = ceil_div(groups * tiles, kAttendPart);
+        p.waves = most < slots ? most : slots;
+        p.parts = p.waves + groups;
+        p.ends_bytes = ceil_div(4 * (tokens + 1), 64) * 64;
+    } else {
+        p.split = ATTEND_CHUNKED;
+        p.chunks = ceil_div(span, kAttendChunk);
+        p.waves = groups * p.chunks;
+        p.parts = p.waves;
+    }
+    p.workspace = p.ends_bytes + p.parts * (n_q_heads / n_kv_heads) * (d + 2) * 4;
     return p;
+}
+
+// Tiles a BALANCED wave takes of `all`.
+constexpr uint32_t attend_part(uint32_t all, uint32_t waves)
+{
+    const uint32_t n = all / waves + (all % waves != 0);
+    return n < (uint32_t)kAttendPart ? (uint32_t)kAttendPart : n;
 }
 
 }  // namespace retopk

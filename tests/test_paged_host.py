@@ -231,6 +231,7 @@ PLAN_PROGRAM = r"""
 #include "retopk_paged_plan.h"
 #include <cstdio>
 #include <initializer_list>
+#include <vector>
 using namespace retopk;
 static int bad(const char *what, long long a, long long b) { printf("%s: %lld %lld\n", what, a, b); return 1; }
 int main()
@@ -247,26 +248,78 @@ int main()
         }
     }
     for (int64_t len = 1; len < ((int64_t)1 << 31); len = len < 600 ? len + 1 : len + len / 3 + 11)
-        for (int64_t tokens : {1, 2, 7, 32, 255, 4096})
+        for (int64_t tokens : {1, 2, 7, 32, 255, 256, 257, 4096})
             for (int64_t hkv : {1, 4, 8, 40})
                 for (int64_t w : {0, 1, 31, 32, 33, 4096, 1 << 30}) {
-                    const AttendPlan p = attend_plan(tokens, hkv * 4, hkv, 128, len, w);
-                    if (p.chunk_rows < 1 || p.chunk_rows % kAttendTile) return bad("rows", len, p.chunk_rows);
-                    if (p.chunks < 1 || p.blocks != tokens * hkv * p.chunks) return bad("blocks", len, p.blocks);
-                    // the positions of a token whose window begins as late in its tile as it can
-                    int64_t worst = len;
+                    const AttendPlan p = attend_plan(tokens, hkv * 4, hkv, 128, len, w, 512);
+                    // tiles of a token whose window begins as late in its tile as it can
+                    int64_t worst = ceil_div(len, kAttendTile);
                     if (w > 0 && w < len) {
                         worst = 0;
                         for (int64_t first = 0; first < 64 && first + w <= len; ++first) {
-                            const int64_t n = first + w - first / kAttendTile * kAttendTile;
+                            const int64_t n = ceil_div(first + w - first / kAttendTile * kAttendTile, kAttendTile);
                             worst = n > worst ? n : worst;
                         }
                     }
-                    if (p.chunks * p.chunk_rows < worst) return bad("covered", len, w);
-                    if ((p.chunks > 1) != (p.workspace > 0)) return bad("workspace", len, p.workspace);
-                    if (p.chunks > 1 && p.workspace < tokens * hkv * 4 * p.chunks * 130 * 4)
-                        return bad("small", len, p.workspace);
+                    if (p.split == ATTEND_DIRECT && (worst > kAttendDirect || p.waves != tokens * hkv || p.workspace))
+                        return bad("direct", len, w);
+                    if (p.split == ATTEND_BALANCED &&
+                        (p.waves < 1 || p.waves > 512 || tokens > kAttendTokens || p.parts != p.waves + tokens * hkv))
+                        return bad("balanced", len, p.waves);
+                    if (p.split == ATTEND_CHUNKED && (p.chunks * kAttendChunk < worst * kAttendTile || p.waves != tokens * hkv * p.chunks))
+                        return bad("chunked", len, p.chunks);
+                    if (p.split != ATTEND_DIRECT && p.workspace < p.ends_bytes + p.parts * 4 * 130 * 4)
+                        return bad("workspace", len, p.workspace);
+                    if (p.ends_bytes % 64 || (p.split == ATTEND_BALANCED && p.ends_bytes < 4 * (tokens + 1)))
+                        return bad("ends", tokens, p.ends_bytes);
                 }
+    // BALANCED: over random lengths, every tile in one part, no number twice, and the numbers the
+    // joining kernel computes are the ones the parts were written to
+    uint32_t seed = 1;
+    auto rnd = [&](uint32_t n) { seed = seed * 1664525u + 1013904223u; return (seed >> 8) % n; };
+    for (int round = 0; round < 4000; ++round) {
+        const int tokens = 1 + rnd(round % 7 ? 12 : 256), hkv = 1 + rnd(9), top = 1 + rnd(round % 3 ? 40 : 5000);
+        std::vector<int> tiles(tokens), ends(tokens);
+        int all = 0, most = 0;
+        for (int t = 0; t < tokens; ++t) {
+            tiles[t] = rnd(4) ? (int)rnd(top + 1) : 0;
+            most = tiles[t] > most ? tiles[t] : most;
+            ends[t] = all += tiles[t] * hkv;
+        }
+        const AttendPlan p = attend_plan(tokens, hkv, hkv, 64, (int64_t)(most < 9 ? 9 : most) * kAttendTile, 0, 1 + rnd(512));
+        if (p.split != ATTEND_BALANCED) return bad("split", tokens, p.split);
+        const int per = (int)attend_part(all, (uint32_t)p.waves);
+        if ((int64_t)per * p.waves < all) return bad("part", per, all);
+        std::vector<int> written(p.parts, -1);
+        std::vector<int> covered(tokens * hkv, 0);
+        for (int64_t b = 0; b < p.waves; ++b)
+            for (int64_t at = b * per; at < (b + 1) * per && at < all;) {
+                int t = 0;
+                while (ends[t] <= at) ++t;
+                const int start = t ? ends[t - 1] : 0, g = (int)(at - start) / tiles[t], first = (int)(at - start) % tiles[t];
+                int64_t n = tiles[t] - first, left = (b + 1) * per < all ? (b + 1) * per - at : all - at;
+                if (n > left) n = left;
+                const int group = t * hkv + g;
+                if (covered[group] != first) return bad("order", group, first);
+                covered[group] += (int)n;
+                if (n != tiles[t]) {
+                    const int64_t id = b + group;
+                    if (id >= p.parts || written[id] >= 0) return bad("number", id, group);
+                    written[id] = group;
+                }
+                at += n;
+            }
+        for (int t = 0; t < tokens; ++t)
+            for (int g = 0; g < hkv; ++g) {
+                const int group = t * hkv + g;
+                if (covered[group] != tiles[t]) return bad("covered", group, covered[group]);
+                const int from = (t ? ends[t - 1] : 0) + g * tiles[t], b0 = from / per;
+                const int b1 = tiles[t] ? (from + tiles[t] - 1) / per : b0 - 1;
+                if (b0 != b1)
+                    for (int b = b0; b <= b1; ++b)
+                        if (written[b + group] != group) return bad("join", b, group);
+            }
+    }
     printf("ok\n");
     return 0;
 }
