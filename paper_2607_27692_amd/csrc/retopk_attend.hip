@@ -142,14 +142,32 @@ __device__ __forceinline__ float out_factor(const Share &w, float l)
     return w.part >= 0 ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
 }
 
-// The plain kernel: D / 8 lanes a row, every position's scores, maximum and weights in
-// turn.  GP >= a.group heads; those past the group repeat its first.
-template <typename T, int D, int GP, int FMT>
-__global__ __launch_bounds__(kAttendThreads) void k_attend(AttendArgs a)
+// ---------------------------------------------------------------------------
+// f32 and bf16 pages
+// ---------------------------------------------------------------------------
+
+// Sum over the LPR lanes (8 or 16, a half or a whole DPP row) that share a position.
+template <int LPR> __device__ __forceinline__ float lanes_sum(float x)
 {
-    constexpr int LPR = D / 8, SLOTS = 64 / LPR;
+    x += dpp_f32<kQuadXor1>(x);
+    x += dpp_f32<kQuadXor2>(x);
+    x += dpp_f32<kHalfMirror>(x);
+    if constexpr (LPR == 16) x += dpp_f32<0x140>(x);   // row_mirror
+    return x;
+}
+
+// k_attend: LPR = D / 8 lanes a position, 8 elements of its key and value rows a lane; a wave
+// takes 64 / LPR positions at once, U times over in a step, whose rows are loaded a step ahead and
+// whose pages are looked up two steps ahead, since any position may be on another page.  All in
+// float32 on the vector units: 8 products and 8 value sums a lane, position and head, which
+// stay below the time HBM needs for the rows.  GP >= a.group heads; those past the group repeat
+// its first.
+template <typename T, int D, int GP>
+__global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
+{
+    constexpr int LPR = D / 8, SLOTS = 64 / LPR, U = 4, STEP = SLOTS * U;
     for_shares(a, [&](const Share &w) {
-        const int lane = threadIdx.x & 63, e0 = lane % LPR * 8;
+        const int lane = threadIdx.x & 63, e0 = lane % LPR * 8, slot = lane / LPR;
         float q[GP][8], acc[GP][8], m[GP], l[GP];
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
@@ -160,38 +178,93 @@ __global__ __launch_bounds__(kAttendThreads) void k_attend(AttendArgs a)
             m[j] = -FLT_MAX;
             l[j] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[j][i] = 0.0f;
+            for (int i = 0; i < 8; ++i) {
+                q[j][i] *= a.scale2;
+                acc[j][i] = 0.0f;
+            }
         }
-        for (int r = max(w.lo, w.span.first) + lane / LPR; r < w.hi; r += SLOTS) {
-            const int64_t row = row_of(a.c, w.seq, r, w.g);
-            if (row < 0) continue;
-            float k[8], v[8];
-            Oct<T> x, y;
-            x.load((const T *)a.c.k + row * D + e0);
-            y.load((const T *)a.c.v + row * D + e0);
-            x.get(k);
-            y.get(v);
+        const int n_it = (w.hi - w.lo + STEP - 1) / STEP;
+        Oct<T> k[U], v[U];
+        int32_t r0[U], r1[U];                          // rows of this step and the next, -1: none
+        auto rows = [&](int it, int32_t (&r)[U]) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int pos = w.lo + it * STEP + u * SLOTS + slot;
+                r[u] = pos >= w.span.first && pos < w.hi ? row_of(a.c, w.seq, pos, w.g) : -1;
+            }
+        };
+        auto load = [&](Oct<T> (&x)[U], const char *from, const int32_t (&r)[U]) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                x[u].load((const T *)from + (uint64_t)(uint32_t)max(r[u], 0) * D + e0);
+        };
+        if (n_it > 0) {
+            rows(0, r0);
+            load(k, a.c.k, r0);
+            load(v, a.c.v, r0);
+            rows(1, r1);
+        }
+        for (int it = 0; it < n_it; ++it) {
+            float s[U][GP];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float x[8];
+                k[u].get(x);
+#pragma unroll
+                for (int j = 0; j < GP; ++j) {
+                    s[u][j] = q[j][0] * x[0];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) s[u][j] = fmaf(q[j][i], x[i], s[u][j]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load(k, a.c.k, r1);                        // past the last step: rows -1, row 0 instead
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < GP; ++j) s[u][j] = r0[u] >= 0 ? lanes_sum<LPR>(s[u][j]) : -INFINITY;
 #pragma unroll
             for (int j = 0; j < GP; ++j) {
-                float s = 0.0f;
+                float mn = m[j];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s = fmaf(q[j][i], k[i], s);
-#pragma unroll
-                for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
-                s *= a.scale2;
-                const float mn = fmaxf(m[j], s), f = exp2f(m[j] - mn), p = exp2f(s - mn);
+                for (int u = 0; u < U; ++u) mn = fmaxf(mn, s[u][j]);
+                const float f = __builtin_amdgcn_exp2f(m[j] - mn);
                 m[j] = mn;
-                l[j] = l[j] * f + p;
+                float sum = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[j][i] = fmaf(p, v[i], acc[j][i] * f);
+                for (int u = 0; u < U; ++u) {
+                    s[u][j] = __builtin_amdgcn_exp2f(s[u][j] - mn);
+                    sum += s[u][j];
+                }
+                l[j] = fmaf(l[j], f, sum);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[j][i] *= f;
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float x[8];
+                v[u].get(x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = r0[u] >= 0 ? x[i] : 0.0f;     // whatever lies in row 0
+#pragma unroll
+                for (int j = 0; j < GP; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[j][i] = fmaf(s[u][j], x[i], acc[j][i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load(v, a.c.v, r1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) r0[u] = r1[u];
+            rows(it + 2, r1);
         }
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
 #pragma unroll
             for (int o = LPR; o < 64; o <<= 1) {
                 const float m2 = __shfl_xor(m[j], o), l2 = __shfl_xor(l[j], o), mn = fmaxf(m[j], m2);
-                const float f = exp2f(m[j] - mn), f2 = exp2f(m2 - mn);
+                const float f = __builtin_amdgcn_exp2f(m[j] - mn), f2 = __builtin_amdgcn_exp2f(m2 - mn);
                 m[j] = mn;
                 l[j] = l[j] * f + l2 * f2;
 #pragma unroll
@@ -654,10 +727,10 @@ __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
     if (lane == 0 && a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
-template <typename T, int D, int FMT> const void *attend_kernel(int group)
+template <typename T, int D> const void *attend_kernel(int group)
 {
-    return group <= 1 ? (const void *)&k_attend<T, D, 1, FMT> : group <= 2 ? (const void *)&k_attend<T, D, 2, FMT>
-           : group <= 4 ? (const void *)&k_attend<T, D, 4, FMT> : (const void *)&k_attend<T, D, 8, FMT>;
+    return group <= 1 ? (const void *)&k_attend<T, D, 1> : group <= 2 ? (const void *)&k_attend<T, D, 2>
+           : group <= 4 ? (const void *)&k_attend<T, D, 4> : (const void *)&k_attend<T, D, 8>;
 }
 template <typename T> const void *attend4_kernel(int d, int group)
 {
@@ -666,8 +739,8 @@ template <typename T> const void *attend4_kernel(int d, int group)
 }
 template <int D> const void *attend_kernel(int format, int dtype, int group)
 {
-    if (format == RETOPK_PAGES_BF16) return attend_kernel<uint16_t, D, RETOPK_PAGES_BF16>(group);
-    if (format == RETOPK_PAGES_F32) return attend_kernel<float, D, RETOPK_PAGES_F32>(group);
+    if (format == RETOPK_PAGES_BF16) return attend_kernel<uint16_t, D>(group);
+    if (format == RETOPK_PAGES_F32) return attend_kernel<float, D>(group);
     return dtype == RETOPK_BF16 ? attend4_kernel<uint16_t>(D, group) : attend4_kernel<float>(D, group);
 }
 
