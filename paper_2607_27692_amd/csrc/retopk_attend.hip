@@ -11,6 +11,8 @@
 namespace retopk {
 namespace {
 
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
 constexpr int kAttendThreads = 64 * kAttendWaves;
 #ifndef AB
 #define AB 2048
@@ -156,16 +158,17 @@ template <int LPR> __device__ __forceinline__ float lanes_sum(float x)
     return x;
 }
 
-// k_attend: LPR = D / 8 lanes a position, 8 elements of its key and value rows a lane; a wave
+// k_attend (f32 pages): LPR = D / 8 lanes a position, 8 elements of its key and value rows a lane; a wave
 // takes 64 / LPR positions at once, U times over in a step, whose rows are loaded a step ahead and
 // whose pages are looked up two steps ahead, since any position may be on another page.  All in
 // float32 on the vector units: 8 products and 8 value sums a lane, position and head, which
 // stay below the time HBM needs for the rows.  GP >= a.group heads; those past the group repeat
 // its first.
-template <typename T, int D, int GP>
+template <int D, int GP>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
 {
-    constexpr int LPR = D / 8, SLOTS = 64 / LPR, U = 4, STEP = SLOTS * U;
+    using T = float;
+    constexpr int LPR = D / 8, SLOTS = 64 / LPR, U = GP == 8 ? 2 : 4, STEP = SLOTS * U;
     for_shares(a, [&](const Share &w) {
         const int lane = threadIdx.x & 63, e0 = lane % LPR * 8, slot = lane / LPR;
         float q[GP][8], acc[GP][8], m[GP], l[GP];
@@ -282,11 +285,195 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
     });
 }
 
+// k_attend16 (bf16 pages): the matrix cores take both products.  A tile is 32 positions; lanes
+// 0 .. 31 look up a position's row each, a tile ahead of its loads, and share the row numbers through
+// LDS, since any position may be on another page.  Scores: 16 positions x 32 elements x 16 columns,
+// lane (col, kq) holding those of positions 4 kq .. + 3 of both halves of the tile for head
+// col % GP.  Values: 16 elements x 32 positions x 16 columns, whose positions are in the order in
+// which a lane already has its weights; pairs of positions are put side by side with byte permutes.
+// A weight is the sum of three bf16 parts (24 bits): column c has part c / GP of head c % GP, for
+// GP = 8 the third in a second product.  Products start from zero and are added by the vector units:
+// accumulated in the matrix cores the sums lose 2^-24 of the largest product at every step.
+template <int D, int GP>
+__global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
+{
+    constexpr int KS = D / 32, NV = D / 16;
+    constexpr int VD = D / 32;                         // dwords of a lane's share of a value row
+    __shared__ __attribute__((aligned(16))) uint32_t s_row[kAttendWaves][2][32];
+    for_shares(a, [&](const Share &w) {
+        const int lane = threadIdx.x & 63, col = lane & 15, kq = lane >> 4;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int hc = col % GP, head = hc < a.group ? hc : 0, part = col / GP;
+        const int n_it = (w.hi - w.lo + 31) / 32;
+
+        bf16x8_t qb[KS];
+        {
+            const u32x4_t *qr = (const u32x4_t *)((const uint16_t *)a.q + w.t * a.q_ts + (w.g * a.group + head) * a.q_hs);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qb[ks] = __builtin_bit_cast(bf16x8_t, qr[ks * 4 + kq]);
+        }
+        // row of position lane % 32 of tile `it`, -1: not attended or no page
+        auto find = [&](int it) {
+            const int pos = w.lo + it * 32 + (lane & 31);
+            return pos >= w.span.first && pos < w.hi ? row_of(a.c, w.seq, pos, w.g) : -1;
+        };
+        // publishes a tile's rows (row 0 for none) and returns which there are
+        auto publish = [&](int it, int32_t row) {
+            if (lane < 32) s_row[wave][it & 1][lane] = (uint32_t)max(row, 0);
+            wave_lds_fence();
+            return (uint32_t)__ballot(row >= 0);
+        };
+        u32x4_t kv[2][KS];
+        uint32_t vv[8][VD];
+        auto load_k = [&](int it) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const u32x4_t *p = (const u32x4_t *)(a.c.k + (uint64_t)s_row[wave][it & 1][16 * u + col] * (2 * D));
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) kv[u][ks] = p[ks * 4 + kq];
+            }
+        };
+        auto load_v = [&](int it) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const u32x4_t r = *(const u32x4_t *)&s_row[wave][it & 1][16 * u + 4 * kq];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const char *p = a.c.v + (uint64_t)r[i] * (2 * D) + col * (D / 8);
+                    if constexpr (VD == 4) {
+                        const u32x4_t x = *(const u32x4_t *)p;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) vv[4 * u + i][e] = x[e];
+                    } else {
+                        const uint2 x = *(const uint2 *)p;
+                        vv[4 * u + i][0] = x.x;
+                        vv[4 * u + i][1] = x.y;
+                    }
+                }
+            }
+        };
+        f32x4_t acc[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        float m = -FLT_MAX, l = 0.0f;
+        const float after1 = part >= 1 ? 1.0f : 0.0f, after2 = part >= 2 ? 1.0f : 0.0f;
+
+        int32_t ahead = n_it > 0 ? find(0) : -1;
+        uint32_t on = publish(0, ahead), on_next = 0u;
+        if (n_it > 0) {
+            load_k(0);
+            load_v(0);
+            ahead = find(1);
+        }
+        for (int it = 0; it < n_it; ++it) {
+            float s[8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                f32x4_t d[KS];
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    d[ks] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv[u][ks]), qb[ks],
+                                                                    f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+                for (int n = KS / 2; n > 0; n /= 2)
+#pragma unroll
+                    for (int ks = 0; ks < n; ++ks) d[ks] += d[ks + n];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * u + i] = d[0][i];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            on_next = publish(it + 1, ahead);          // past the last tile: none, row 0 is loaded
+            load_k(it + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (on != 0xFFFFFFFFu) {
+                asm volatile("");                      // a branch, not selects in every tile
+                const uint32_t mine = on >> (4 * kq);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool there = mine >> (16 * (i >> 2) + (i & 3)) & 1u;
+                    s[i] = there ? s[i] : -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < VD; ++e) vv[i][e] = there ? vv[i][e] : 0u;   // whatever lies there
+                }
+            }
+            float tm = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) tm = fmaxf(tm, s[i]);
+            tm = max_rows_f32(tm) * a.scale2;
+            // the reference moves by steps, as in k_attend4
+            if (__ballot(tm > m + 1.0f) != 0ull) {
+                const float mn = tm > m + 1.0f ? tm + 1.0f : m, f = __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) acc[j] *= f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -m));
+                l += s[i];
+            }
+            // this column's part of the weights; the third one too
+            u32x4_t pb, pc;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x2_t x = {s[2 * i], s[2 * i + 1]};
+                const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2_t));
+                const f32x2_t y = {fmaf(-bf16_lo(h), GP == 4 ? after1 : 1.0f, x[0]), fmaf(-bf16_hi(h), GP == 4 ? after1 : 1.0f, x[1])};
+                const uint32_t h2 = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2_t));
+                if constexpr (GP == 4) {
+                    const f32x2_t z = {fmaf(-bf16_lo(h2), after2, y[0]), fmaf(-bf16_hi(h2), after2, y[1])};
+                    pb[i] = part < 3 ? __builtin_bit_cast(uint32_t, __builtin_convertvector(z, bf16x2_t)) : 0u;
+                } else {
+                    const f32x2_t z = {y[0] - bf16_lo(h2), y[1] - bf16_hi(h2)};
+                    pb[i] = part == 0 ? h : h2;
+                    pc[i] = part == 0 ? __builtin_bit_cast(uint32_t, __builtin_convertvector(z, bf16x2_t)) : 0u;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                u32x4_t x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    x[i] = __builtin_amdgcn_perm(vv[2 * i + 1][j / 2], vv[2 * i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+                f32x4_t d = {0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (GP == 8)
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, pc), d, 0, 0, 0);
+                acc[j] += __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, pb), d, 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(it + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            on = on_next;
+            ahead = it + 2 < n_it ? find(it + 2) : -1;
+        }
+        l = add16_f32(l, l);
+        l = add32_f32(l, l);
+        if (lane < GP && hc < a.group) write_sum(a, w, hc, m, l);
+        // rows 4 kq + i of product j are elements (4 kq + i) * NV + j; a head's parts lie GP columns apart
+        const float f = out_factor(w, l);
+        float *out = (w.part < 0 ? a.out : a.part_o) + w.row(a, hc) * D + 4 * kq * NV;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j0 = 0; j0 < NV; j0 += 4) {
+                f32x4_t o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    o[j] = acc[j0 + j][i];
+                    o[j] += row_ror_f32(o[j], 8);
+                    if constexpr (GP == 4) o[j] += row_ror_f32(o[j], 4);
+                    o[j] *= f;
+                }
+                if (col < GP && hc < a.group) *(f32x4_t *)(out + i * NV + j0) = o;
+            }
+    });
+}
+
 // ---------------------------------------------------------------------------
 // 4-bit pages
 // ---------------------------------------------------------------------------
 
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
@@ -727,10 +914,10 @@ __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
     if (lane == 0 && a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
-template <typename T, int D> const void *attend_kernel(int group)
+template <int D> const void *attend_f32_kernel(int group)
 {
-    return group <= 1 ? (const void *)&k_attend<T, D, 1> : group <= 2 ? (const void *)&k_attend<T, D, 2>
-           : group <= 4 ? (const void *)&k_attend<T, D, 4> : (const void *)&k_attend<T, D, 8>;
+    return group <= 1 ? (const void *)&k_attend<D, 1> : group <= 2 ? (const void *)&k_attend<D, 2>
+           : group <= 4 ? (const void *)&k_attend<D, 4> : (const void *)&k_attend<D, 8>;
 }
 template <typename T> const void *attend4_kernel(int d, int group)
 {
@@ -739,8 +926,9 @@ template <typename T> const void *attend4_kernel(int d, int group)
 }
 template <int D> const void *attend_kernel(int format, int dtype, int group)
 {
-    if (format == RETOPK_PAGES_BF16) return attend_kernel<uint16_t, D>(group);
-    if (format == RETOPK_PAGES_F32) return attend_kernel<float, D>(group);
+    if (format == RETOPK_PAGES_BF16)
+        return group <= 4 ? (const void *)&k_attend16<D, 4> : (const void *)&k_attend16<D, 8>;
+    if (format == RETOPK_PAGES_F32) return attend_f32_kernel<D>(group);
     return dtype == RETOPK_BF16 ? attend4_kernel<uint16_t>(D, group) : attend4_kernel<float>(D, group);
 }
 
