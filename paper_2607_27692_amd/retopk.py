@@ -159,10 +159,23 @@ def _addr(x):
     return x.data_ptr()
 
 
+_CURRENT_STREAM = None
+
+
+def _current_stream():
+    """torch's current stream of the current device, by the call torch's own generated code
+    makes where there is one: torch.cuda.current_stream() builds an object, 3 us a call."""
+    global _CURRENT_STREAM
+    import torch
+    if _CURRENT_STREAM is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _CURRENT_STREAM = (lambda d: torch.cuda.current_stream(d).cuda_stream) if raw is None else raw
+    return _CURRENT_STREAM(torch.cuda.current_device())
+
+
 def _stream(s):
     if s is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -324,64 +337,74 @@ def make_rope(rot_dim, theta=10000.0, interleaved=False, scaling="none", factor=
 
 
 _NO_ROWS = retopk_rows(None, 0, 0)
+_DTYPE_OF = {}              # torch dtype: retopk_dtype
 
 
 def _dtype_of(fn: str, name: str, x) -> int:
-    es = x.element_size()
-    if es == 4 and not str(x.dtype).endswith("int32"):
-        return RETOPK_F32
-    if es == 2 and not str(x.dtype).endswith("float16") or str(x.dtype).endswith("bfloat16"):
-        return RETOPK_BF16
-    raise RetopkError(fn, -1, f"{name} is {x.dtype}: float32 or bfloat16 expected")
+    """float32 or bfloat16 (or the bits of one, int16)."""
+    if not _DTYPE_OF:
+        import torch
+        _DTYPE_OF.update({torch.float32: RETOPK_F32, torch.bfloat16: RETOPK_BF16,
+                          torch.int16: RETOPK_BF16})
+    got = _DTYPE_OF.get(x.dtype)
+    if got is None:
+        raise RetopkError(fn, -1, f"{name} is {x.dtype}: float32 or bfloat16 expected")
+    return got
 
 
-def _rows(fn: str, name: str, x, tokens=None, heads=None, d=None, like=None) -> retopk_rows:
-    """A [tokens, heads, d] GPU tensor whose last dimension is dense, of these sizes."""
-    if not x.is_cuda:
-        raise RetopkError(fn, -1, f"{name} is not a GPU tensor")
-    if x.dim() != 3:
-        raise RetopkError(fn, -1, f"{name} has {x.dim()} dimensions, [tokens, heads, d] expected")
-    want = tuple(a if b is None else b for a, b in zip(x.shape, (tokens, heads, d)))
-    if tuple(x.shape) != want:
-        raise RetopkError(fn, -1, f"{name} has shape {tuple(x.shape)}, {want} expected")
-    if like is not None and (x.dtype != like.dtype or x.device != like.device):
-        raise RetopkError(fn, -1, f"{name} is {x.dtype} on {x.device}, {like.dtype} on "
-                                  f"{like.device} expected")
+def _rows(fn: str, name: str, x, shape, dtype, dev: int) -> retopk_rows:
+    """A [tokens, heads, d] tensor of this shape and type on this device, whose last dimension
+    is dense."""
+    if x.shape != shape or x.dtype != dtype or x.get_device() != dev:
+        raise RetopkError(fn, -1, f"{name} is {x.dtype} {list(x.shape)} on {x.device}: {dtype} "
+                                  f"{list(shape)} on GPU {dev} expected")
     ts, hs, es = x.stride()
     if es != 1:
         raise RetopkError(fn, -1, f"{name}: its last dimension is not dense")
     # the stride of a dimension of one element is never used
-    return retopk_rows(x.data_ptr(), 0 if want[0] == 1 else ts, 0 if want[1] == 1 else hs)
+    return retopk_rows(x.data_ptr(), 0 if shape[0] == 1 else ts, 0 if shape[1] == 1 else hs)
 
 
-def _index(fn: str, name: str, x, n: int, like):
-    """A dense int32 GPU tensor of n elements on the device of `like`."""
-    if x.dtype.itemsize != 4 or x.is_floating_point():
-        raise RetopkError(fn, -1, f"{name} is {x.dtype}: int32 expected")
-    if x.device != like.device or not x.is_contiguous() or x.numel() != n:
-        raise RetopkError(fn, -1, f"{name}: {n} dense elements on {like.device} expected")
+def _first(fn: str, name: str, x, heads=None, d=None):
+    """Checks the tensor that the others of a call are to be like; its shape, type and device."""
+    if x.dim() != 3 or not x.is_cuda:
+        raise RetopkError(fn, -1, f"{name}: a [tokens, heads, d] GPU tensor expected")
+    shape = x.shape
+    if heads is not None and shape[1] != heads or d is not None and shape[2] != d:
+        raise RetopkError(fn, -1, f"{name} has shape {list(shape)}, [tokens, {heads or 'heads'}, {d}] "
+                                  "expected")
+    return shape, x.dtype, x.get_device()
+
+
+def _index(fn: str, name: str, x, n: int, dev: int):
+    """A dense int32 GPU tensor of n elements."""
+    if x.numel() != n or x.element_size() != 4 or x.is_floating_point() or \
+            x.get_device() != dev or not x.is_contiguous():
+        raise RetopkError(fn, -1, f"{name}: {n} dense int32 elements on GPU {dev} expected")
     return x.data_ptr()
 
 
-def _launch(name: str, device, stream, *args):
+def _launch(name: str, dev: int, stream, *args):
     """Calls a library function with the device of its tensors current."""
     import torch
-    fn = getattr(load(), name)
-    if device.index == torch.cuda.current_device():
-        _check(name, fn(*args, _stream(stream)))
+    fn = getattr(_LIB or load(), name)
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, _stream(stream))
     else:
-        with torch.cuda.device(device):
-            _check(name, fn(*args, _stream(stream)))
+        with torch.cuda.device(dev):
+            rc = fn(*args, _stream(stream))
+    if rc:
+        _check(name, rc)
 
 
 def rotary_embed(rope: retopk_rope, x, pos, out, inverse=False, stream=None) -> None:
     """out = x [tokens, heads, d] rotated to the int32 positions pos [tokens]; with inverse,
     the gradient of x for the gradient x of out.  out may be x."""
-    rx = _rows("rotary_embed", "x", x)
-    t, h, d = x.shape
-    ro = _rows("rotary_embed", "out", out, t, h, d, x)
-    _launch("rotary_embed", x.device, stream, C.byref(rope), _dtype_of("rotary_embed", "x", x), d,
-            h, t, _index("rotary_embed", "pos", pos, t, x), rx, ro, 1 if inverse else 0)
+    fn = "rotary_embed"
+    shape, dt, dev = _first(fn, "x", x)
+    _launch(fn, dev, stream, C.byref(rope), _dtype_of(fn, "x", x), shape[2], shape[1], shape[0],
+            _index(fn, "pos", pos, shape[0], dev), _rows(fn, "x", x, shape, dt, dev),
+            _rows(fn, "out", out, shape, dt, dev), 1 if inverse else 0)
 
 
 class PagedCache:
@@ -419,7 +442,8 @@ class PagedCache:
         fmt = RETOPK_PAGES_Q4 if self.q4 else {RETOPK_F32: RETOPK_PAGES_F32,
                                                RETOPK_BF16: RETOPK_PAGES_BF16}[_dtype_of(fn, "k", k)]
         self.tensors = (k, v, table, k_par, v_par)
-        self.k, self.device, self.n_kv_heads, self.head_dim = k, k.device, hkv, d
+        self.device, self.n_kv_heads, self.head_dim = k.device, hkv, d
+        self.dev = k.get_device()
         self.c = retopk_pages(fmt, hkv, d, page, n, table.shape[0], table.shape[1], k.data_ptr(),
                               v.data_ptr(), k_par.data_ptr() if self.q4 else None,
                               v_par.data_ptr() if self.q4 else None, table.data_ptr())
@@ -446,6 +470,10 @@ class PagedCache:
     def table(self):
         return self.tensors[2]
 
+    @property
+    def k(self):
+        return self.tensors[0]
+
     def workspace(self, n_tokens, n_q_heads, max_len, window=0):
         """A workspace for paged_attention calls of these sizes, None where it needs none."""
         import torch
@@ -458,21 +486,24 @@ def paged_append(cache: PagedCache, seq, pos, k, v, rope: retopk_rope | None = N
     """Rows t of k and v [tokens, Hkv, d] to positions pos[t] of sequences seq[t], k rotated on
     the way when rope is given; q [tokens, Hq, d], rotated, to q_out."""
     fn = "paged_append"
-    rk = _rows(fn, "k", k, None, cache.n_kv_heads, cache.head_dim)
-    t = k.shape[0]
-    rv = _rows(fn, "v", v, t, cache.n_kv_heads, cache.head_dim, k)
+    shape, dt, dev = _first(fn, "k", k, cache.n_kv_heads, cache.head_dim)
+    t = shape[0]
+    if dev != cache.dev:
+        raise RetopkError(fn, -1, f"k is on {k.device}, the cache on {cache.device}")
     hq, rq, ro = 0, _NO_ROWS, _NO_ROWS
     if q is not None:
         if q_out is None:
             raise RetopkError(fn, -1, "q without q_out")
-        rq = _rows(fn, "q", q, t, None, cache.head_dim, k)
-        hq = q.shape[1]
-        ro = _rows(fn, "q_out", q_out, t, hq, cache.head_dim, k)
-    if k.device != cache.device:
-        raise RetopkError(fn, -1, f"k is on {k.device}, the cache on {cache.device}")
-    _launch(fn, k.device, stream, C.byref(cache.c), C.byref(rope) if rope is not None else None,
-            _dtype_of(fn, "k", k), t, _index(fn, "seq", seq, t, k), _index(fn, "pos", pos, t, k),
-            rk, rv, hq, rq, ro)
+        q_shape = _first(fn, "q", q, None, cache.head_dim)[0]
+        if q_shape[0] != t:
+            raise RetopkError(fn, -1, f"q has {q_shape[0]} tokens, k {t}")
+        hq = q_shape[1]
+        rq = _rows(fn, "q", q, q_shape, dt, dev)
+        ro = _rows(fn, "q_out", q_out, q_shape, dt, dev)
+    _launch(fn, dev, stream, C.byref(cache.c), C.byref(rope) if rope is not None else None,
+            _dtype_of(fn, "k", k), t, _index(fn, "seq", seq, t, dev),
+            _index(fn, "pos", pos, t, dev), _rows(fn, "k", k, shape, dt, dev),
+            _rows(fn, "v", v, shape, dt, dev), hq, rq, ro)
 
 
 def paged_gather(cache: PagedCache, seq, pos, k=None, v=None, stream=None) -> None:
@@ -481,13 +512,15 @@ def paged_gather(cache: PagedCache, seq, pos, k=None, v=None, stream=None) -> No
     first = k if k is not None else v
     if first is None:
         return
-    t, h, d = seq.numel(), cache.n_kv_heads, cache.head_dim
-    if first.device != cache.device:
+    shape, dt, dev = _first(fn, "k" if k is not None else "v", first, cache.n_kv_heads,
+                            cache.head_dim)
+    t = shape[0]
+    if dev != cache.dev:
         raise RetopkError(fn, -1, f"k or v is on {first.device}, the cache on {cache.device}")
-    rk = _rows(fn, "k", k, t, h, d) if k is not None else _NO_ROWS
-    rv = _rows(fn, "v", v, t, h, d, first) if v is not None else _NO_ROWS
-    _launch(fn, first.device, stream, C.byref(cache.c), _dtype_of(fn, "k", first), t,
-            _index(fn, "seq", seq, t, first), _index(fn, "pos", pos, t, first), rk, rv)
+    rk = _rows(fn, "k", k, shape, dt, dev) if k is not None else _NO_ROWS
+    rv = _rows(fn, "v", v, shape, dt, dev) if v is not None else _NO_ROWS
+    _launch(fn, dev, stream, C.byref(cache.c), _dtype_of(fn, "k", first), t,
+            _index(fn, "seq", seq, t, dev), _index(fn, "pos", pos, t, dev), rk, rv)
 
 
 def paged_attention_workspace(cache: PagedCache, n_tokens, n_q_heads, max_len, window=0) -> int:
@@ -515,20 +548,23 @@ def paged_attention(cache: PagedCache, seq, pos, q, out, max_len, window=0, lse=
     [tokens, Hq, d] and lse [tokens, Hq] are float32.  workspace: PagedCache.workspace of the
     same sizes (None: a new one; hold one for graphs, and one a graph)."""
     fn = "paged_attention"
-    rq = _rows(fn, "q", q, None, None, cache.head_dim)
-    t, hq = q.shape[0], q.shape[1]
-    if q.device != cache.device:
+    shape, dt, dev = _first(fn, "q", q, None, cache.head_dim)
+    t, hq = shape[0], shape[1]
+    if dev != cache.dev:
         raise RetopkError(fn, -1, f"q is on {q.device}, the cache on {cache.device}")
     for name, x, n in (("out", out, t * hq * cache.head_dim), ("lse", lse, t * hq)):
-        if x is not None:
-            _check_tensor(fn, name, x, n, 4)
-            if not x.is_floating_point() or x.device != q.device:
-                raise RetopkError(fn, -1, f"{name}: float32 on {q.device} expected")
+        if x is not None and (x.element_size() != 4 or not x.is_floating_point() or
+                              x.numel() != n or x.get_device() != dev or not x.is_contiguous()):
+            raise RetopkError(fn, -1, f"{name}: {n} dense float32 elements on {q.device} expected")
     if workspace is None:
         workspace = _workspace_on(cache, t, hq, max_len, window, stream)
-    _launch(fn, q.device, stream, C.byref(cache.c), _dtype_of(fn, "q", q), t, hq,
-            _index(fn, "seq", seq, t, q), _index(fn, "pos", pos, t, q), rq, max_len, window,
-            out.data_ptr(), _addr(lse), _addr(workspace),
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise RetopkError(fn, -1, f"workspace: a dense tensor on {q.device} expected")
+    _launch(fn, dev, stream, C.byref(cache.c), _dtype_of(fn, "q", q), t, hq,
+            _index(fn, "seq", seq, t, dev), _index(fn, "pos", pos, t, dev),
+            _rows(fn, "q", q, shape, dt, dev), max_len, window, out.data_ptr(),
+            None if lse is None else lse.data_ptr(),
+            None if workspace is None else workspace.data_ptr(),
             0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
