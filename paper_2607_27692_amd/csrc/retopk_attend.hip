@@ -59,6 +59,7 @@ struct Share {
     int g, seq, lo, hi;
     Span span;
     int64_t part;
+    bool joint;                // the block's four waves share the group and join their results
     // row of head j of the group in the output or among the partial results
     __device__ __forceinline__ int64_t row(const AttendArgs &a, int j) const
     {
@@ -77,6 +78,8 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
     const int worker = blockIdx.x * kAttendWaves + __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool balanced = a.split == ATTEND_BALANCED;
     int at = 0, last = worker < a.waves ? 1 : 0;
+    int64_t block_from = 0, block_to = 0;      // the block's tiles
+    bool whole_block = false;                  // all of its waves have theirs
     if (balanced) {
         // every token's last tile (of all KV heads), counted by each block for itself
         const int sq = tid < a.n_tokens ? a.seq[tid] : -1, p = tid < a.n_tokens ? a.pos[tid] : -1;
@@ -95,6 +98,9 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
         const int64_t from = (int64_t)worker * per;
         at = (int)min(from, (int64_t)all);
         last = (int)min(from + per, (int64_t)all);
+        block_from = (int64_t)blockIdx.x * kAttendWaves * per;
+        block_to = block_from + kAttendWaves * per;
+        whole_block = block_to <= (int64_t)all;
     }
     while (at < last) {
         Share w;
@@ -115,7 +121,9 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
             w.span = span_of(a, w.seq, __builtin_amdgcn_readfirstlane(s_pos[t]));
             w.lo = w.span.base + first * kAttendTile;
             w.hi = min(w.span.len, w.lo + step * kAttendTile);
-            w.part = step == tiles ? -1 : (int64_t)worker + (int64_t)t * hkv + w.g;
+            const int base = start + w.g * tiles;      // the group's first tile
+            w.joint = whole_block && block_from >= base && block_to <= base + tiles;
+            w.part = step == tiles ? -1 : (int64_t)(w.joint ? blockIdx.x * kAttendWaves : worker) + (int64_t)t * hkv + w.g;
         } else {
             const int chunk = worker % a.chunks, bg = worker / a.chunks;
             w.t = bg / hkv;
@@ -125,6 +133,7 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
             w.lo = w.span.base + chunk * kAttendChunk;
             w.hi = min(w.span.len, w.lo + kAttendChunk);
             w.part = a.split == ATTEND_DIRECT ? -1 : (int64_t)worker;
+            w.joint = false;
             if (a.split == ATTEND_DIRECT) w.hi = w.span.len;
         }
         if (w.lo < w.hi || w.part < 0) f(w);
@@ -132,17 +141,53 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
     }
 }
 
-// The weights' sum l and reference m of head j of a share; what its value sums are times.
-__device__ __forceinline__ void write_sum(const AttendArgs &a, const Share &w, int j, float m, float l)
-{
-    const int64_t row = w.row(a, j);
-    if (w.part >= 0) a.part_ml[row] = make_float2(m, l);
-    else if (a.lse) a.lse[row] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
-}
-__device__ __forceinline__ float out_factor(const Share &w, float l)
-{
-    return w.part >= 0 ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
-}
+// Where a wave leaves its result: shared memory for waves that join theirs, else the output or
+// a partial result.
+template <int D, int GP> struct Joint {
+    float o[kAttendWaves][GP][D], m[kAttendWaves][GP], l[kAttendWaves][GP];
+
+    __device__ __forceinline__ float *row(const AttendArgs &a, const Share &w, int j)
+    {
+        return w.joint ? o[threadIdx.x >> 6][j] : (w.part < 0 ? a.out : a.part_o) + w.row(a, j) * D;
+    }
+    // the weights' sum and reference of head j, and what the value sums are times
+    __device__ __forceinline__ void sum(const AttendArgs &a, const Share &w, int j, float mj, float lj)
+    {
+        if (w.joint) {
+            m[threadIdx.x >> 6][j] = mj;
+            l[threadIdx.x >> 6][j] = lj;
+        } else if (w.part >= 0) {
+            a.part_ml[w.row(a, j)] = make_float2(mj, lj);
+        } else if (a.lse) {
+            a.lse[w.row(a, j)] = lj > 0.0f ? (mj + log2f(lj)) * kLn2 : -INFINITY;
+        }
+    }
+    static __device__ __forceinline__ float factor(const Share &w, float lj)
+    {
+        return w.part >= 0 ? 1.0f : lj > 0.0f ? 1.0f / lj : 0.0f;
+    }
+    // at a share's end, by every wave of the block if any joins
+    __device__ __forceinline__ void finish(const AttendArgs &a, const Share &w)
+    {
+        if (!w.joint) return;
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.group * D; i += kAttendThreads) {
+            const int j = i / D, e = i % D;
+            float mx = m[0][j], x = 0.0f, lj = 0.0f;
+#pragma unroll
+            for (int v = 1; v < kAttendWaves; ++v) mx = fmaxf(mx, m[v][j]);
+#pragma unroll
+            for (int v = 0; v < kAttendWaves; ++v) {
+                const float f = __builtin_amdgcn_exp2f(m[v][j] - mx);
+                x = fmaf(f, o[v][j][e], x);
+                lj = fmaf(f, l[v][j], lj);
+            }
+            const int64_t to = w.row(a, j);
+            a.part_o[to * D + e] = x;
+            if (e == 0) a.part_ml[to] = make_float2(mx, lj);
+        }
+    }
+};
 
 // ---------------------------------------------------------------------------
 // f32 and bf16 pages
@@ -169,6 +214,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
 {
     using T = float;
     constexpr int LPR = D / 8, SLOTS = 64 / LPR, U = GP == 8 ? 2 : 4, STEP = SLOTS * U;
+    __shared__ __attribute__((aligned(16))) Joint<D, GP> s_join;
     for_shares(a, [&](const Share &w) {
         const int lane = threadIdx.x & 63, e0 = lane % LPR * 8, slot = lane / LPR;
         float q[GP][8], acc[GP][8], m[GP], l[GP];
@@ -274,14 +320,14 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
                 for (int i = 0; i < 8; ++i) acc[j][i] = acc[j][i] * f + __shfl_xor(acc[j][i], o) * f2;
             }
             if (lane < LPR && j < a.group) {
-                const float f = out_factor(w, l[j]);
-                float *o = (w.part < 0 ? a.out : a.part_o) + w.row(a, j) * D + e0;
+                const float f = s_join.factor(w, l[j]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[j][i] *= f;
-                Oct<float>::store(o, acc[j]);
-                if (lane == 0) write_sum(a, w, j, m[j], l[j]);
+                Oct<float>::store(s_join.row(a, w, j) + e0, acc[j]);
+                if (lane == 0) s_join.sum(a, w, j, m[j], l[j]);
             }
         }
+        s_join.finish(a, w);
     });
 }
 
@@ -300,6 +346,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
     constexpr int KS = D / 32, NV = D / 16;
     constexpr int VD = D / 32;                         // dwords of a lane's share of a value row
     __shared__ __attribute__((aligned(16))) uint32_t s_row[kAttendWaves][2][32];
+    __shared__ __attribute__((aligned(16))) Joint<D, GP> s_join;
     for_shares(a, [&](const Share &w) {
         const int lane = threadIdx.x & 63, col = lane & 15, kq = lane >> 4;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -449,10 +496,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
         }
         l = add16_f32(l, l);
         l = add32_f32(l, l);
-        if (lane < GP && hc < a.group) write_sum(a, w, hc, m, l);
+        if (lane < GP && hc < a.group) s_join.sum(a, w, hc, m, l);
         // rows 4 kq + i of product j are elements (4 kq + i) * NV + j; a head's parts lie GP columns apart
-        const float f = out_factor(w, l);
-        float *out = (w.part < 0 ? a.out : a.part_o) + w.row(a, hc) * D + 4 * kq * NV;
+        const float f = s_join.factor(w, l);
+        float *out = s_join.row(a, w, hc) + 4 * kq * NV;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -467,6 +514,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
                 }
                 if (col < GP && hc < a.group) *(f32x4_t *)(out + i * NV + j0) = o;
             }
+        s_join.finish(a, w);
     });
 }
 
@@ -536,6 +584,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
     constexpr int NV = D / 16;                 // value products: codes of a lane's share of a row
     constexpr int NQ = sizeof(T) == 4 ? 2 : 1; // float16 parts of the query
     static_assert(PACK || NG == 2, "d = 64 always packs");
+    __shared__ __attribute__((aligned(16))) Joint<D, 8> s_join;
     for_shares(a, [&](const Share &w) {
     const int g = w.g, lo = w.lo, hi = w.hi;
     const int lane = threadIdx.x & 63, col = lane & 15, kq = lane >> 4;
@@ -817,11 +866,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
     l = add32_f32(l, l);
     z = add16_f32(z, z);
     z = add32_f32(z, z);
-    if (lane < 8 && gr == 0 && hc < a.group) write_sum(a, w, hc, m, l);
+    if (lane < 8 && gr == 0 && hc < a.group) s_join.sum(a, w, hc, m, l);
     // rows 4 kq + i of product j are elements (4 kq + i) * (D / 16) + j, right in the columns of
     // their own group
-    const float f = out_factor(w, l);
-    float *out = (w.part < 0 ? a.out : a.part_o) + w.row(a, hc) * D + 4 * kq * (D / 16);
+    const float f = s_join.factor(w, l);
+    float *out = s_join.row(a, w, hc) + 4 * kq * (D / 16);
     const bool mine = !(PACK && col >= 8) && (NG == 1 || (kq >> 1) == gr) && hc < a.group;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -836,6 +885,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
             }
             if (mine) *(f32x4_t *)(out + i * (D / 16) + j0) = o;
         }
+    s_join.finish(a, w);
     });
 }
 
@@ -852,21 +902,27 @@ __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
     const int h = (int)(row % a.n_q), g = h / a.group;
     int64_t part;
     int nch;
+    // parts `lead` .. lead + joints - 1 are blocks', every kAttendWaves-th number, the others waves'
+    int lead = 0, joints = 0;
     if (a.split == ATTEND_BALANCED) {
         const int per = a.ends[a.n_tokens], start = t > 0 ? a.ends[t - 1] : 0;
         const int tiles = (a.ends[t] - start) / a.c.n_kv_heads, from = start + g * tiles;
-        const int b0 = from / per, b1 = tiles > 0 ? (from + tiles - 1) / per : b0 - 1;
-        if (b0 == b1) return;      // all in one block, which wrote the output
-        nch = b1 - b0 + 1;
-        part = b0 + t * a.c.n_kv_heads + g;
+        const AttendParts p = attend_parts(from, from + tiles, per);
+        if (p.count == 1 && p.joints == 0) return;     // all in one wave, which wrote the output
+        nch = p.count;
+        lead = p.lead;
+        joints = p.joints;
+        part = p.first + t * a.c.n_kv_heads + g;
     } else {
         nch = (span_of(a, a.seq[t], a.pos[t]).tiles() + kAttendChunk / kAttendTile - 1) / (kAttendChunk / kAttendTile);
         part = (t * a.c.n_kv_heads + g) * a.chunks;
     }
-    part = part * a.group + (h - g * a.group);
+    const int j = h - g * a.group;
+    auto place = [&](int c) {
+        const int extra = c < lead ? 0 : c < lead + joints ? c - lead : joints;
+        return (part + c + extra * (kAttendWaves - 1)) * a.group + j;
+    };
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
-    const float2 *ml = a.part_ml + part;
-    const float *po = a.part_o + part * D + lane * E;
     float m = -FLT_MAX, l = 0.0f, o[E] = {};
     for (int c0 = wave * U; c0 < nch; c0 += waves * U) {
         float2 x[U];
@@ -874,9 +930,10 @@ __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = min(c0 + u, nch - 1);
-            x[u] = ml[(int64_t)c * a.group];
+            const int64_t at = place(c);
+            x[u] = a.part_ml[at];
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[u][e] = po[(int64_t)c * a.group * D + e];
+            for (int e = 0; e < E; ++e) v[u][e] = a.part_o[at * D + lane * E + e];
         }
         float mn = m;
 #pragma unroll
@@ -1010,8 +1067,15 @@ retopk_status paged_attention(const retopk_pages *c, int32_t dtype, int64_t n_to
         return RETOPK_ERR_HIP;
     if (p.split != ATTEND_DIRECT) {
         f = d == 64 ? (const void *)&k_attend_merge<64> : (const void *)&k_attend_merge<128>;
-        // waves for the parts of a group four times as long as the mean, at most
-        const int64_t parts = ceil_div(4 * p.parts, n_tokens * c->n_kv_heads), need = ceil_div(parts, kMergeUnroll);
+        // waves for the parts of a group that is almost all there is, or of twice the mean one: more
+        // would be idle in most blocks (32 sequences, 28 heads: 10.7 us with 9 waves a block)
+        int64_t most = p.chunks;
+        if (p.split == ATTEND_BALANCED) {
+            most = ceil_div(p.waves, kAttendWaves * c->n_kv_heads) + 2 * kAttendWaves;
+            const int64_t twice = 2 * ceil_div(p.waves, n_tokens * c->n_kv_heads) + 2 * kAttendWaves;
+            most = most < twice ? most : twice;
+        }
+        const int64_t need = ceil_div(most, kMergeUnroll);
         const int64_t waves = need < kMergeWaves ? need : kMergeWaves;
         if (hipLaunchKernel(f, dim3((unsigned)(n_tokens * n_q_heads)), dim3((unsigned)(64 * waves)), args, 0, s) != hipSuccess)
             return RETOPK_ERR_HIP;

@@ -41,7 +41,8 @@ constexpr uint32_t divide(uint32_t x, Divisor d)
 //   CHUNKED   wave (token, KV head, chunk of kAttendChunk rows) for more tokens than that;
 //             waves past a sequence's end leave at once.
 // The partial results of BALANCED have numbers wave + group, which no two parts share (each
-// part of a wave begins a new group, each part of a group a new wave).
+// part of a wave begins a new group, each part of a group a new wave).  Where all waves of a
+// block work on one group they join their results under the number of the first.
 constexpr int kAttendTile = 32;       // positions of a tile
 constexpr int kAttendDirect = 8;      // tiles
 constexpr int kAttendPart = 2;        // fewest tiles of a BALANCED wave
@@ -89,6 +90,21 @@ constexpr uint32_t attend_part(uint32_t all, uint32_t waves)
 {
     const uint32_t n = all / waves + (all % waves != 0);
     return n < (uint32_t)kAttendPart ? (uint32_t)kAttendPart : n;
+}
+
+// The parts of a group whose tiles are [from, to), `per` a wave: waves from `first` on, of which
+// after `lead` there are `joints` whole blocks that joined theirs.
+struct AttendParts {
+    int first, count, lead, joints;
+};
+constexpr AttendParts attend_parts(int from, int to, int per)
+{
+    const int b0 = from / per, b1 = to > from ? (to - 1) / per : b0 - 1;
+    const int64_t block = (int64_t)kAttendWaves * per;
+    const int k0 = (int)((from + block - 1) / block), k1 = (int)(to / block);
+    if (k1 <= k0) return AttendParts{b0, b1 - b0 + 1, 0, 0};
+    const int lead = kAttendWaves * k0 - b0;
+    return AttendParts{b0, lead + (k1 - k0) + (b1 - kAttendWaves * k1 + 1), lead, k1 - k0};
 }
 
 }  // namespace retopk

@@ -291,7 +291,7 @@ int main()
         const int per = (int)attend_part(all, (uint32_t)p.waves);
         if ((int64_t)per * p.waves < all) return bad("part", per, all);
         std::vector<int> written(p.parts, -1);
-        std::vector<int> covered(tokens * hkv, 0);
+        std::vector<int> covered(tokens * hkv, 0), parts(tokens * hkv, 0);
         for (int64_t b = 0; b < p.waves; ++b)
             for (int64_t at = b * per; at < (b + 1) * per && at < all;) {
                 int t = 0;
@@ -303,8 +303,13 @@ int main()
                 if (covered[group] != first) return bad("order", group, first);
                 covered[group] += (int)n;
                 if (n != tiles[t]) {
-                    const int64_t id = b + group;
-                    if (id >= p.parts || written[id] >= 0) return bad("number", id, group);
+                    // the four waves of a block inside the group have one part together
+                    const int64_t block = b / kAttendWaves * kAttendWaves, base = start + (int64_t)g * tiles[t];
+                    const bool joint = block * per >= base && (block + kAttendWaves) * per <= base + tiles[t];
+                    const int64_t id = (joint ? block : b) + group;
+                    if (id >= p.parts || (written[id] >= 0 && !(joint && written[id] == group && b != block)))
+                        return bad("number", id, group);
+                    if (!joint || b == block) parts[group] += 1;
                     written[id] = group;
                 }
                 at += n;
@@ -313,11 +318,19 @@ int main()
             for (int g = 0; g < hkv; ++g) {
                 const int group = t * hkv + g;
                 if (covered[group] != tiles[t]) return bad("covered", group, covered[group]);
-                const int from = (t ? ends[t - 1] : 0) + g * tiles[t], b0 = from / per;
-                const int b1 = tiles[t] ? (from + tiles[t] - 1) / per : b0 - 1;
-                if (b0 != b1)
-                    for (int b = b0; b <= b1; ++b)
-                        if (written[b + group] != group) return bad("join", b, group);
+                const int from = (t ? ends[t - 1] : 0) + g * tiles[t];
+                const AttendParts q = attend_parts(from, from + tiles[t], per);
+                if (q.count == 1 && q.joints == 0) {   // one wave, which writes the output
+                    if (parts[group]) return bad("direct", group, parts[group]);
+                    continue;
+                }
+                if (q.count != parts[group]) return bad("count", q.count, parts[group]);
+                for (int c = 0; c < q.count; ++c) {
+                    const int extra = c < q.lead ? 0 : c < q.lead + q.joints ? c - q.lead : q.joints;
+                    const int64_t id = q.first + group + c + extra * (kAttendWaves - 1);
+                    if (id >= p.parts || written[id] != group) return bad("join", id, group);
+                    written[id] = -2;
+                }
             }
     }
     printf("ok\n");
