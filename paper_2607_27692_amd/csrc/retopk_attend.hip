@@ -11,8 +11,6 @@
 namespace retopk {
 namespace {
 
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-
 constexpr int kAttendThreads = 64 * kAttendWaves;
 #ifndef AB
 #define AB 2048

@@ -39,13 +39,14 @@ __device__ __forceinline__ int32_t row_of(const PagesArgs &c, int32_t s, int32_t
     return (page * c.n_kv_heads + g) * c.page_size + (p - (int32_t)at * c.page_size);
 }
 
-// bf16 bits of x, round to nearest even (finite x; NaN stays NaN in value, not in bits).
-__device__ __forceinline__ uint32_t bf16_bits(float x)
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// bf16 bits of x, and of two values side by side, rounded to nearest even.
+__device__ __forceinline__ uint32_t bf16_pair(float x, float y)
 {
-    const uint32_t u = __float_as_uint(x);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (u >> 16) | 0x40u;
-    return (u + ((u >> 16) & 1u) + 0x7FFFu) >> 16;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x, y}), bf16x2_t));
 }
+__device__ __forceinline__ uint32_t bf16_bits(float x) { return bf16_pair(x, 0.0f); }
 
 // Elements of type T (float, or uint16_t for bf16) as 8 floats, and back.
 template <typename T> struct Oct;
@@ -92,7 +93,7 @@ template <> struct Oct<uint16_t> {
     {
         u32x4_t u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = bf16_bits(x[2 * i]) | (bf16_bits(x[2 * i + 1]) << 16);
+        for (int i = 0; i < 4; ++i) u[i] = bf16_pair(x[2 * i], x[2 * i + 1]);
         *(u32x4_t *)p = u;
     }
     static __device__ __forceinline__ float one(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }

@@ -96,8 +96,47 @@ template <typename T> Rows<T> rows_of(const retopk_rows &x) { return Rows<T>{(T 
 // The rotation of one lane's 8 elements
 // ---------------------------------------------------------------------------
 
-// Cosines and sines of a block's tokens, one angle a thread at a time: pos * freq in
-// float64, whose reduction keeps every bit that float32 results show at any position.
+// sin and cos of x in float64: x less a multiple n of pi/2 (its nearest double and the rest of
+// it, each times n in one rounding), then the Taylor series about 0, whose first terms left out
+// are below 2^-58 for |r| <= pi/4; the quadrant n mod 4 says which of the two is which.  Past
+// 2^28, where n times the rest of pi/2 would no longer be small, the library's.
+__device__ __forceinline__ void angle(double x, double &s, double &c)
+{
+    if (!(fabs(x) < 268435456.0)) {
+        sincos(x, &s, &c);
+        return;
+    }
+    const double n = rint(x * 0.63661977236758134308);
+    double r = fma(-n, 1.5707963267948965580, x);
+    r = fma(-n, 6.1232339957367658861e-17, r);
+    const double z = r * r;
+    double p = 1.0 / 355687428096000.0;                        // 1 / 17!
+    p = fma(p, z, -1.0 / 1307674368000.0);
+    p = fma(p, z, 1.0 / 6227020800.0);
+    p = fma(p, z, -1.0 / 39916800.0);
+    p = fma(p, z, 1.0 / 362880.0);
+    p = fma(p, z, -1.0 / 5040.0);
+    p = fma(p, z, 1.0 / 120.0);
+    p = fma(p, z, -1.0 / 6.0);
+    const double sr = fma(p * z, r, r);
+    double q = 1.0 / 20922789888000.0;                         // 1 / 16!
+    q = fma(q, z, -1.0 / 87178291200.0);
+    q = fma(q, z, 1.0 / 479001600.0);
+    q = fma(q, z, -1.0 / 3628800.0);
+    q = fma(q, z, 1.0 / 40320.0);
+    q = fma(q, z, -1.0 / 720.0);
+    q = fma(q, z, 1.0 / 24.0);
+    q = fma(q, z, -0.5);
+    const double cr = fma(q, z, 1.0);
+    const int k = (int)n;
+    s = k & 1 ? cr : sr;
+    c = k & 1 ? sr : cr;
+    if (k & 2) s = -s;
+    if ((k + 1) & 2) c = -c;
+}
+
+// Cosines and sines of a block's tokens, a few angles a thread: pos * freq in float64, which
+// keeps every bit that float32 results show at any position.
 template <int D>
 __device__ __forceinline__ void block_angles(const retopk_rope &r, const int32_t *pos, int64_t t0, int64_t n,
                                              bool inverse, double2 *s_cs)
@@ -108,7 +147,7 @@ __device__ __forceinline__ void block_angles(const retopk_rope &r, const int32_t
         const int tok = i / (D / 2), pair = i % (D / 2);
         if (pair < half && t0 + tok < n) {
             double s, c;
-            sincos((double)pos[t0 + tok] * r.freq[pair], &s, &c);
+            angle((double)pos[t0 + tok] * r.freq[pair], s, c);
             s_cs[i] = make_double2(c * r.factor, (inverse ? -s : s) * r.factor);
         }
     }
@@ -118,38 +157,39 @@ __device__ __forceinline__ void block_angles(const retopk_rope &r, const int32_t
 // x[i] * c[i] + partner * s[i], the partner being the other element of its pair.
 template <typename T, int D> struct Turn {
     double c[8], s[8];
-    int e0, half, rot, interleaved;
+    int e0, half, rot, other;  // other: where the partners of a whole lane begin
+    bool inside, lanes;        // partners in the lane itself; or all in one other lane
 
     __device__ __forceinline__ void init(const retopk_rope &r, const double2 *cs, int lane_e0)
     {
         e0 = lane_e0;
         rot = r.rot_dim;
         half = rot / 2;
-        interleaved = r.interleaved;
+        inside = r.interleaved != 0;
+        lanes = !inside && half % 8 == 0;
+        other = e0 < half ? e0 + half : e0 < rot ? e0 - half : e0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int e = e0 + i;
             c[i] = 1.0;
             s[i] = 0.0;
             if (e < rot) {
-                const int pair = interleaved ? e / 2 : (e < half ? e : e - half);
-                const bool first = interleaved ? (e % 2 == 0) : e < half;
+                const int pair = inside ? e / 2 : (e < half ? e : e - half);
+                const bool first = inside ? (e % 2 == 0) : e < half;
                 const double2 v = cs[pair];
                 c[i] = v.x;
                 s[i] = first ? -v.y : v.y;
             }
         }
     }
-    // The partners of a row's elements e0 ..; x holds the elements themselves.
-    __device__ __forceinline__ void partners(const T *row, const float (&x)[8], float (&y)[8]) const
+    __device__ __forceinline__ void turn(const T *row, const Oct<T> &partner, float (&x)[8]) const
     {
-        if (interleaved) {
+        float y[8];
+        if (inside) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
-        } else if (half % 8 == 0) {           // whole lanes trade places
-            Oct<T> v;
-            v.load(row + (e0 < half ? e0 + half : e0 < rot ? e0 - half : e0));
-            v.get(y);
+        } else if (lanes) {
+            partner.get(y);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -157,18 +197,47 @@ template <typename T, int D> struct Turn {
                 y[i] = Oct<T>::one(row + (e < half ? e + half : e < rot ? e - half : e));
             }
         }
-    }
-    __device__ __forceinline__ void turn(float (&x)[8], const float (&y)[8]) const
-    {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (e0 + i < rot) x[i] = (float)((double)x[i] * c[i] + (double)y[i] * s[i]);
+        for (int i = 0; i < 8; ++i) {
+            const float z = (float)fma((double)x[i], c[i], (double)y[i] * s[i]);
+            x[i] = e0 + i < rot ? z : x[i];
+        }
     }
 };
 
-// rotary_embed.  Block (x, y): tokens x * TT .., heads y * per_block ..  In place: a row's
-// lanes are in one wave, and its loads, partners included, have all returned before its
-// stores.
+// Walks a token's rows first .. last - 1, kAhead of them loaded ahead of their use: at(h) is row
+// h, and f(h, x) takes its elements, turned if h < n_rot.  In place: a row's lanes are in one wave,
+// and its loads, partners included, have all returned before its stores.
+constexpr int kAhead = 4;
+template <typename T, int D, typename At, typename F>
+__device__ __forceinline__ void walk_rows(const Turn<T, D> &turn, int e0, int first, int last, int n_rot, At at, F f)
+{
+    Oct<T> own[kAhead], partner[kAhead];
+    auto load = [&](int h, Oct<T> &a, Oct<T> &b) {
+        const T *row = at(h < last ? h : last - 1);
+        a.load(row + e0);
+        if (h < n_rot && turn.lanes) b.load(row + turn.other);
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load(first + u, own[u], partner[u]);
+    for (int h0 = first; h0 < last; h0 += kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int h = h0 + u;
+            if (h < last) {
+                float x[8];
+                own[u].get(x);
+                if (h < n_rot) turn.turn(at(h), partner[u], x);
+                __builtin_amdgcn_sched_barrier(0);
+                load(h + kAhead, own[u], partner[u]);
+                __builtin_amdgcn_sched_barrier(0);
+                f(h, x);
+            }
+        }
+    }
+}
+
+// rotary_embed.  Block (x, y): tokens x * TT .., heads y * per_block ..
 template <typename T, int D>
 __global__ __launch_bounds__(kRowThreads) void k_rotary(retopk_rope r, Rows<T> x, Rows<T> out, const int32_t *pos,
                                                         int64_t n, int heads, int per_block, int inverse)
@@ -183,17 +252,9 @@ __global__ __launch_bounds__(kRowThreads) void k_rotary(retopk_rope r, Rows<T> x
     if (t >= n) return;
     Turn<T, D> turn;
     turn.init(r, s_cs[tok], e0);
-    const int h1 = min(heads, ((int)blockIdx.y + 1) * per_block);
-    for (int h = blockIdx.y * per_block; h < h1; ++h) {
-        const T *row = x.at(t, h);
-        Oct<T> v;
-        float a[8], b[8];
-        v.load(row + e0);
-        v.get(a);
-        turn.partners(row, a, b);
-        turn.turn(a, b);
-        Oct<T>::store(out.at(t, h) + e0, a);
-    }
+    const int h0 = blockIdx.y * per_block, h1 = min(heads, h0 + per_block);
+    walk_rows(turn, e0, h0, h1, heads, [&](int h) { return (const T *)x.at(t, h); },
+              [&](int h, const float (&v)[8]) { Oct<T>::store(out.at(t, h) + e0, v); });
 }
 
 // ---------------------------------------------------------------------------
@@ -202,9 +263,9 @@ __global__ __launch_bounds__(kRowThreads) void k_rotary(retopk_rope r, Rows<T> x
 
 // A lane's 8 elements as codes of its group (8 lanes side by side); the parameter word is
 // the same in every lane of the group.  mid and scale are rounded to bf16, the nearest
-// steps at half the bytes of float32; the code is exact for them: the candidate from
-// float32 arithmetic is put right by comparisons in float64, where j * scale and x - mid
-// are exact.
+// steps at half the bytes of float32.  The code is exact for them: the number of whole scales
+// from the bottom, mid - 8 scale, is at most one short when the reciprocal is rounded towards
+// zero, which the remainder shows; bottom, remainder and comparison are exact in float64.
 __device__ __forceinline__ void quantise4(const float (&x)[8], uint32_t &codes, uint32_t &par)
 {
     float top = x[0], low = x[0];
@@ -223,25 +284,22 @@ __device__ __forceinline__ void quantise4(const float (&x)[8], uint32_t &codes, 
     const double mid = (double)__uint_as_float(mid_b << 16);
     const double up = (double)top - mid, down = mid - (double)low;
     const uint32_t scale_b = bf16_bits((float)((up > down ? up : down) / 7.5));
-    const float scale_f = __uint_as_float(scale_b << 16);
-    const double scale = (double)scale_f;
+    const double scale = (double)__uint_as_float(scale_b << 16), bottom = fma(-8.0, scale, mid);
     par = scale_b | (mid_b << 16);
-    const double inv = scale > 0.0 ? 1.0 / scale : 0.0;
-    codes = 0u;
+    // scale 0: any code stands for mid
+    const double step = scale > 0.0 ? scale : INFINITY, inv = scale > 0.0 ? (1.0 / scale) * (1.0 - 0x1p-50) : 0.0;
+    uint32_t w[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const double d = (double)x[i] - mid;
-        // floor(d / scale), at most one off before the comparisons
-        double f = floor(d * inv);
-        const double rest = fma(-f, scale, d);
-        if (rest < 0.0) f -= 1.0;
-        else if (rest >= scale && scale > 0.0) f += 1.0;
-        const int n = (int)fmin(fmax(f, -8.0), 7.0);
-        const uint32_t s = n < 0 ? 1u : 0u, m = (uint32_t)(n < 0 ? -1 - n : n);
+        const double d = (double)x[i] - bottom, f = floor(d * inv);
+        const int whole = (int)f + (fma(-f, scale, d) >= step ? 1 : 0);
+        const int c = min(max(whole, 0), 15) - 8;              // c + 1/2 scales from mid
+        const uint32_t m = (uint32_t)(c ^ (c >> 31));          // |c + 1/2| - 1/2
         // elements 0 .. 3 of a half-word: magnitude and sign bit places
         const int mp[4] = {4, 0, 12, 8}, sp[4] = {15, 11, 7, 3};
-        codes |= ((m << mp[i & 3]) | (s << sp[i & 3])) << (16 * (i >> 2));
+        w[i >> 2] |= (m << mp[i & 3]) | ((uint32_t)c & (1u << 31) ? 1u << sp[i & 3] : 0u);
     }
+    codes = w[0] | (w[1] << 16);
 }
 
 template <int FMT, int D>
@@ -283,23 +341,20 @@ __global__ __launch_bounds__(kRowThreads) void k_append(PagesArgs c, retopk_rope
     const int32_t row0 = row_of(c, s, pos[t], 0);
     Turn<T, D> turn;
     if (h0 < n_rot) turn.init(r, s_cs[tok], e0);
-    for (int h = h0; h < h1; ++h) {
-        const int kind = h < n_q ? 0 : h < n_q + c.n_kv_heads ? 1 : 2;
-        const int g = kind == 0 ? h : kind == 1 ? h - n_q : h - n_q - c.n_kv_heads;
-        const T *src = kind == 0 ? q.at(t, g) : kind == 1 ? k.at(t, g) : v.at(t, g);
-        Oct<T> o;
-        float a[8], b[8];
-        o.load(src + e0);
-        o.get(a);
-        if (h < n_rot) {
-            turn.partners(src, a, b);
-            turn.turn(a, b);
-        }
-        if (kind == 0)
-            Oct<T>::store(q_out.at(t, g) + e0, a);
-        else
-            store_row<FMT, D>(c, kind == 1, row0 < 0 ? -1 : row0 + g * c.page_size, e0, a);
-    }
+    walk_rows(turn, e0, h0, h1, n_rot,
+              [&](int h) {
+                  return (const T *)(h < n_q ? q.at(t, h) : h < n_q + c.n_kv_heads ? k.at(t, h - n_q)
+                                                                                   : v.at(t, h - n_q - c.n_kv_heads));
+              },
+              [&](int h, const float (&x)[8]) {
+                  if (h < n_q) {
+                      Oct<T>::store(q_out.at(t, h) + e0, x);
+                  } else {
+                      const bool key = h < n_q + c.n_kv_heads;
+                      const int g = h - n_q - (key ? 0 : c.n_kv_heads);
+                      store_row<FMT, D>(c, key, row0 < 0 ? -1 : row0 + g * c.page_size, e0, x);
+                  }
+              });
 }
 
 // paged_gather.
