@@ -71,7 +71,7 @@ namespace {
 
 constexpr int kRowThreads = 256;
 // Blocks that keep the chip's memory busy; a block walks over as many heads as that leaves.
-constexpr int64_t kRowBlocks = 2048;
+constexpr int64_t kRowBlocks = 1024;
 constexpr int64_t kMaxGrid = ((int64_t)1 << 31) - 1;
 
 bool rope_ok(const retopk_rope *r, int d)
@@ -205,31 +205,38 @@ template <typename T, int D> struct Turn {
     }
 };
 
-// Walks a token's rows first .. last - 1, kAhead of them loaded ahead of their use: at(h) is row
-// h, and f(h, x) takes its elements, turned if h < n_rot.  In place: a row's lanes are in one wave,
-// and its loads, partners included, have all returned before its stores.
-constexpr int kAhead = 4;
+// Walks a token's rows first .. last - 1, from `start` on and round to it, kAhead of them loaded
+// ahead of their use: at(h) is row h, and f(h, x) takes its elements, turned if h < n_rot.  In place:
+// a row's lanes are in one wave, and its loads, partners included, have all returned before
+// its stores.
+constexpr int kAhead = 2;
 template <typename T, int D, typename At, typename F>
-__device__ __forceinline__ void walk_rows(const Turn<T, D> &turn, int e0, int first, int last, int n_rot, At at, F f)
+__device__ __forceinline__ void walk_rows(const Turn<T, D> &turn, int e0, int first, int last, int start, int n_rot, At at, F f)
 {
     Oct<T> own[kAhead], partner[kAhead];
-    auto load = [&](int h, Oct<T> &a, Oct<T> &b) {
-        const T *row = at(h < last ? h : last - 1);
+    const int count = last - first;
+    auto nth = [&](int i) {
+        const int h = start + min(i, count - 1);
+        return h < last ? h : h - count;
+    };
+    auto load = [&](int i, Oct<T> &a, Oct<T> &b) {
+        const int h = nth(i);
+        const T *row = at(h);
         a.load(row + e0);
         if (h < n_rot && turn.lanes) b.load(row + turn.other);
     };
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) load(first + u, own[u], partner[u]);
-    for (int h0 = first; h0 < last; h0 += kAhead) {
+    for (int u = 0; u < kAhead; ++u) load(u, own[u], partner[u]);
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int h = h0 + u;
-            if (h < last) {
+            const int h = nth(i0 + u);
+            if (i0 + u < count) {
                 float x[8];
                 own[u].get(x);
                 if (h < n_rot) turn.turn(at(h), partner[u], x);
                 __builtin_amdgcn_sched_barrier(0);
-                load(h + kAhead, own[u], partner[u]);
+                load(i0 + u + kAhead, own[u], partner[u]);
                 __builtin_amdgcn_sched_barrier(0);
                 f(h, x);
             }
@@ -253,7 +260,7 @@ __global__ __launch_bounds__(kRowThreads) void k_rotary(retopk_rope r, Rows<T> x
     Turn<T, D> turn;
     turn.init(r, s_cs[tok], e0);
     const int h0 = blockIdx.y * per_block, h1 = min(heads, h0 + per_block);
-    walk_rows(turn, e0, h0, h1, heads, [&](int h) { return (const T *)x.at(t, h); },
+    walk_rows(turn, e0, h0, h1, h0, heads, [&](int h) { return (const T *)x.at(t, h); },
               [&](int h, const float (&v)[8]) { Oct<T>::store(out.at(t, h) + e0, v); });
 }
 
@@ -341,7 +348,10 @@ __global__ __launch_bounds__(kRowThreads) void k_append(PagesArgs c, retopk_rope
     const int32_t row0 = row_of(c, s, pos[t], 0);
     Turn<T, D> turn;
     if (h0 < n_rot) turn.init(r, s_cs[tok], e0);
-    walk_rows(turn, e0, h0, h1, n_rot,
+    // blocks begin a quarter of their heads apart, so that some write queries while others are
+    // busy with codes
+    const int start = h0 + (int)(blockIdx.x & 3) * (h1 - h0) / 4;
+    walk_rows(turn, e0, h0, h1, start, n_rot,
               [&](int h) {
                   return (const T *)(h < n_q ? q.at(t, h) : h < n_q + c.n_kv_heads ? k.at(t, h - n_q)
                                                                                    : v.at(t, h - n_q - c.n_kv_heads));
