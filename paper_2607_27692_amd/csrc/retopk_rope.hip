@@ -270,9 +270,10 @@ __global__ __launch_bounds__(kRowThreads) void k_rotary(retopk_rope r, Rows<T> x
 
 // A lane's 8 elements as codes of its group (8 lanes side by side); the parameter word is
 // the same in every lane of the group.  mid and scale are rounded to bf16, the nearest
-// steps at half the bytes of float32.  The code is exact for them: the number of whole scales
-// from the bottom, mid - 8 scale, is at most one short when the reciprocal is rounded towards
-// zero, which the remainder shows; bottom, remainder and comparison are exact in float64.
+// steps at half the bytes of float32.  With a = |x - mid| / scale the magnitude is the whole part
+// of a, and for x below mid the largest whole number below a, so that the levels are half open:
+// a is taken 2^-48 too small there and 2^-48 too large above, more than its roundings and less
+// than the distance of a quotient of these types from a whole number it does not equal.
 __device__ __forceinline__ void quantise4(const float (&x)[8], uint32_t &codes, uint32_t &par)
 {
     float top = x[0], low = x[0];
@@ -290,21 +291,23 @@ __device__ __forceinline__ void quantise4(const float (&x)[8], uint32_t &codes, 
     const uint32_t mid_b = bf16_bits((float)(((double)top + (double)low) * 0.5));
     const double mid = (double)__uint_as_float(mid_b << 16);
     const double up = (double)top - mid, down = mid - (double)low;
-    const uint32_t scale_b = bf16_bits((float)((up > down ? up : down) / 7.5));
-    const double scale = (double)__uint_as_float(scale_b << 16), bottom = fma(-8.0, scale, mid);
+    const uint32_t scale_b = bf16_bits((float)((up > down ? up : down) * (1.0 / 7.5)));
+    const double scale = (double)__uint_as_float(scale_b << 16);
     par = scale_b | (mid_b << 16);
-    // scale 0: any code stands for mid
-    const double step = scale > 0.0 ? scale : INFINITY, inv = scale > 0.0 ? (1.0 / scale) * (1.0 - 0x1p-50) : 0.0;
+    // 1 / scale by two Newton steps, 2^-48 too small; scale 0: 0, any code stands for mid
+    double inv = scale > 0.0 ? __builtin_amdgcn_rcp(scale) : 0.0;
+    inv = fma(fma(-scale, inv, 1.0), inv, inv);
+    inv = fma(fma(-scale, inv, 1.0), inv, inv) * (1.0 - 0x1p-48);
     uint32_t w[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const double d = (double)x[i] - bottom, f = floor(d * inv);
-        const int whole = (int)f + (fma(-f, scale, d) >= step ? 1 : 0);
-        const int c = min(max(whole, 0), 15) - 8;              // c + 1/2 scales from mid
-        const uint32_t m = (uint32_t)(c ^ (c >> 31));          // |c + 1/2| - 1/2
+        const double d = (double)x[i] - mid;
+        const bool below = d < 0.0;
+        const double a = fabs(d) * inv * (below ? 1.0 : 1.0 + 0x1p-47);
+        const uint32_t m = min((uint32_t)a, 7u);
         // elements 0 .. 3 of a half-word: magnitude and sign bit places
         const int mp[4] = {4, 0, 12, 8}, sp[4] = {15, 11, 7, 3};
-        w[i >> 2] |= (m << mp[i & 3]) | ((uint32_t)c & (1u << 31) ? 1u << sp[i & 3] : 0u);
+        w[i >> 2] |= (m << mp[i & 3]) | (below ? 1u << sp[i & 3] : 0u);
     }
     codes = w[0] | (w[1] << 16);
 }
