@@ -12,10 +12,9 @@ namespace retopk {
 namespace {
 
 constexpr int kAttendThreads = 64 * kAttendWaves;
-#ifndef AB
-#define AB 2048
-#endif
-constexpr int kAttendSlots = AB;    // two waves a SIMD
+// Waves that run at once: two a SIMD by the registers of most builds, three of the 4-bit one of
+// d = 64 (32 ragged sequences: 26.3 us with 3072 waves, 29.3 with 2048; the others lose by more).
+inline int64_t attend_slots(int format, int d) { return format == RETOPK_PAGES_Q4 && d == 64 ? 3072 : 2048; }
 constexpr float kLn2 = 0.69314718055994530942f;
 
 struct AttendArgs {
@@ -69,9 +68,9 @@ struct Share {
 template <typename F>
 __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
 {
+    constexpr int TPT = kAttendTokens / kAttendThreads;        // tokens a thread
     __shared__ int s_ends[kAttendTokens], s_seq[kAttendTokens], s_pos[kAttendTokens];
     __shared__ uint32_t s_red[kAttendWaves];
-    static_assert(kAttendTokens == kAttendThreads, "a token a thread");
     const int hkv = a.c.n_kv_heads, tid = threadIdx.x, lane = tid & 63;
     const int worker = blockIdx.x * kAttendWaves + __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool balanced = a.split == ATTEND_BALANCED;
@@ -80,18 +79,25 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
     bool whole_block = false;                  // all of its waves have theirs
     if (balanced) {
         // every token's last tile (of all KV heads), counted by each block for itself
-        const int sq = tid < a.n_tokens ? a.seq[tid] : -1, p = tid < a.n_tokens ? a.pos[tid] : -1;
-        const int n = span_of(a, sq, p).tiles() * hkv;
-        uint32_t all;
-        const int end = (int)block_excl_scan<kAttendThreads>((uint32_t)n, s_red, &all) + n;
-        const int per = (int)attend_part(all, (uint32_t)a.waves);
-        s_ends[tid] = end;
-        s_seq[tid] = sq;
-        s_pos[tid] = p;
-        if (blockIdx.x == 0 && tid < a.n_tokens) {
-            a.ends[tid] = end;
-            if (tid == 0) a.ends[a.n_tokens] = per;
+        int sum = 0, ends[TPT];
+#pragma unroll
+        for (int i = 0; i < TPT; ++i) {
+            const int t = tid * TPT + i;
+            const int sq = t < a.n_tokens ? a.seq[t] : -1, p = t < a.n_tokens ? a.pos[t] : -1;
+            s_seq[t] = sq;
+            s_pos[t] = p;
+            ends[i] = sum += span_of(a, sq, p).tiles() * hkv;
         }
+        uint32_t all;
+        const int before = (int)block_excl_scan<kAttendThreads>((uint32_t)sum, s_red, &all);
+        const int per = (int)attend_part(all, (uint32_t)a.waves);
+#pragma unroll
+        for (int i = 0; i < TPT; ++i) {
+            const int t = tid * TPT + i;
+            s_ends[t] = before + ends[i];
+            if (blockIdx.x == 0 && t < a.n_tokens) a.ends[t] = before + ends[i];
+        }
+        if (blockIdx.x == 0 && tid == 0) a.ends[a.n_tokens] = per;
         __syncthreads();
         const int64_t from = (int64_t)worker * per;
         at = (int)min(from, (int64_t)all);
@@ -123,18 +129,19 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
             w.joint = whole_block && block_from >= base && block_to <= base + tiles;
             w.part = step == tiles ? -1 : (int64_t)(w.joint ? blockIdx.x * kAttendWaves : worker) + (int64_t)t * hkv + w.g;
         } else {
+            const bool direct = a.split == ATTEND_DIRECT;
             const int chunk = worker % a.chunks, bg = worker / a.chunks;
             w.t = bg / hkv;
             w.g = bg % hkv;
             w.seq = __builtin_amdgcn_readfirstlane(a.seq[w.t]);
             w.span = span_of(a, w.seq, __builtin_amdgcn_readfirstlane(a.pos[w.t]));
-            w.lo = w.span.base + chunk * kAttendChunk;
-            w.hi = min(w.span.len, w.lo + kAttendChunk);
-            w.part = a.split == ATTEND_DIRECT ? -1 : (int64_t)worker;
-            w.joint = false;
-            if (a.split == ATTEND_DIRECT) w.hi = w.span.len;
+            const int rows = direct ? (w.span.tiles() + kAttendWaves - 1) / kAttendWaves * kAttendTile : kAttendChunk;
+            w.lo = w.span.base + chunk * rows;
+            w.hi = min(w.span.len, w.lo + rows);
+            w.part = direct ? -1 : (int64_t)worker;
+            w.joint = direct;
         }
-        if (w.lo < w.hi || w.part < 0) f(w);
+        if (w.lo < w.hi || w.joint) f(w);
         at += step;
     }
 }
@@ -162,7 +169,7 @@ template <int D, int GP> struct Joint {
     }
     static __device__ __forceinline__ float factor(const Share &w, float lj)
     {
-        return w.part >= 0 ? 1.0f : lj > 0.0f ? 1.0f / lj : 0.0f;
+        return w.joint || w.part >= 0 ? 1.0f : lj > 0.0f ? 1.0f / lj : 0.0f;
     }
     // at a share's end, by every wave of the block if any joins
     __device__ __forceinline__ void finish(const AttendArgs &a, const Share &w)
@@ -181,8 +188,13 @@ template <int D, int GP> struct Joint {
                 lj = fmaf(f, l[v][j], lj);
             }
             const int64_t to = w.row(a, j);
-            a.part_o[to * D + e] = x;
-            if (e == 0) a.part_ml[to] = make_float2(mx, lj);
+            if (w.part >= 0) {
+                a.part_o[to * D + e] = x;
+                if (e == 0) a.part_ml[to] = make_float2(mx, lj);
+            } else {
+                a.out[to * D + e] = lj > 0.0f ? x / lj : 0.0f;
+                if (e == 0 && a.lse) a.lse[to] = lj > 0.0f ? (mx + log2f(lj)) * kLn2 : -INFINITY;
+            }
         }
     }
 };
@@ -212,33 +224,45 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
 {
     using T = float;
     constexpr int LPR = D / 8, SLOTS = 64 / LPR, U = GP == 8 ? 2 : 4, STEP = SLOTS * U;
+    constexpr bool QL = GP == 8;                       // the queries in LDS: registers hold no 8 heads' more
+    __shared__ __attribute__((aligned(16))) float s_q[kAttendWaves][QL ? GP : 1][D];
     __shared__ __attribute__((aligned(16))) Joint<D, GP> s_join;
     for_shares(a, [&](const Share &w) {
         const int lane = threadIdx.x & 63, e0 = lane % LPR * 8, slot = lane / LPR;
-        float q[GP][8], acc[GP][8], m[GP], l[GP];
+        const int wave = threadIdx.x >> 6;
+        float q[QL ? 1 : GP][8], acc[GP][8], m[GP], l[GP];
 #pragma unroll
         for (int j = 0; j < GP; ++j) {
             const int h = w.g * a.group + (j < a.group ? j : 0);
             Oct<T> v;
+            float x[8];
             v.load((const T *)a.q + w.t * a.q_ts + h * a.q_hs + e0);
-            v.get(q[j]);
+            v.get(x);
             m[j] = -FLT_MAX;
             l[j] = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                q[j][i] *= a.scale2;
+                x[i] *= a.scale2;
+                if constexpr (!QL) q[j][i] = x[i];
                 acc[j][i] = 0.0f;
             }
+            if constexpr (QL) Oct<float>::store(&s_q[wave][j][e0], x);     // the same from every slot
         }
+        if constexpr (QL) wave_lds_fence();
         const int n_it = (w.hi - w.lo + STEP - 1) / STEP;
         Oct<T> k[U], v[U];
         int32_t r0[U], r1[U];                          // rows of this step and the next, -1: none
-        auto rows = [&](int it, int32_t (&r)[U]) {
+        int32_t pages[U];                              // of the step after
+        auto look = [&](int it) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int pos = w.lo + it * STEP + u * SLOTS + slot;
-                r[u] = pos >= w.span.first && pos < w.hi ? row_of(a.c, w.seq, pos, w.g) : -1;
+                pages[u] = pos >= w.span.first && pos < w.hi ? page_of(a.c, w.seq, pos) : -1;
             }
+        };
+        auto rows = [&](int it, int32_t (&r)[U]) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) r[u] = row_on(a.c, pages[u], w.lo + it * STEP + u * SLOTS + slot, w.g);
         };
         auto load = [&](Oct<T> (&x)[U], const char *from, const int32_t (&r)[U]) {
 #pragma unroll
@@ -246,22 +270,32 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
                 x[u].load((const T *)from + (uint64_t)(uint32_t)max(r[u], 0) * D + e0);
         };
         if (n_it > 0) {
+            look(0);
             rows(0, r0);
+            look(1);
             load(k, a.c.k, r0);
             load(v, a.c.v, r0);
             rows(1, r1);
         }
         for (int it = 0; it < n_it; ++it) {
+            look(it + 2);
             float s[U][GP];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float x[8];
-                k[u].get(x);
+            for (int j = 0; j < GP; ++j) {
+                float y[8];
+                if constexpr (QL) {
+                    wave_lds_fence();                  // read here, not held in registers over the loop
+                    Oct<float> o;
+                    o.load(&s_q[wave][j][e0]);
+                    o.get(y);
+                }
 #pragma unroll
-                for (int j = 0; j < GP; ++j) {
-                    s[u][j] = q[j][0] * x[0];
+                for (int u = 0; u < U; ++u) {
+                    float x[8];
+                    k[u].get(x);
+                    s[u][j] = 0.0f;
 #pragma unroll
-                    for (int i = 1; i < 8; ++i) s[u][j] = fmaf(q[j][i], x[i], s[u][j]);
+                    for (int i = 0; i < 8; ++i) s[u][j] = fmaf(QL ? y[i] : q[QL ? 0 : j][i], x[i], s[u][j]);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -326,6 +360,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
             }
         }
         s_join.finish(a, w);
+        if constexpr (QL) wave_lds_fence();            // the queries of the next share
     });
 }
 
@@ -357,11 +392,12 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) qb[ks] = __builtin_bit_cast(bf16x8_t, qr[ks * 4 + kq]);
         }
-        // row of position lane % 32 of tile `it`, -1: not attended or no page
-        auto find = [&](int it) {
+        // page of position lane % 32 of tile `it`, and its row there; -1: not attended or no page
+        auto look = [&](int it) {
             const int pos = w.lo + it * 32 + (lane & 31);
-            return pos >= w.span.first && pos < w.hi ? row_of(a.c, w.seq, pos, w.g) : -1;
+            return pos >= w.span.first && pos < w.hi ? page_of(a.c, w.seq, pos) : -1;
         };
+        auto row_in = [&](int it, int32_t page) { return row_on(a.c, page, w.lo + it * 32 + (lane & 31), w.g); };
         // publishes a tile's rows (row 0 for none) and returns which there are
         auto publish = [&](int it, int32_t row) {
             if (lane < 32) s_row[wave][it & 1][lane] = (uint32_t)max(row, 0);
@@ -403,14 +439,17 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
         float m = -FLT_MAX, l = 0.0f;
         const float after1 = part >= 1 ? 1.0f : 0.0f, after2 = part >= 2 ? 1.0f : 0.0f;
 
-        int32_t ahead = n_it > 0 ? find(0) : -1;
-        uint32_t on = publish(0, ahead), on_next = 0u;
+        uint32_t on = 0u, on_next = 0u;
+        int32_t ahead = -1;
         if (n_it > 0) {
+            const int32_t first = look(0), second = look(1);
+            on = publish(0, row_in(0, first));
             load_k(0);
             load_v(0);
-            ahead = find(1);
+            ahead = row_in(1, second);
         }
         for (int it = 0; it < n_it; ++it) {
+            const int32_t page = look(it + 2);
             float s[8];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -490,7 +529,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
             load_v(it + 1);
             __builtin_amdgcn_sched_barrier(0);
             on = on_next;
-            ahead = it + 2 < n_it ? find(it + 2) : -1;
+            ahead = row_in(it + 2, page);
         }
         l = add16_f32(l, l);
         l = add32_f32(l, l);
@@ -998,7 +1037,8 @@ retopk_status plan_of(const retopk_pages &c, int64_t n_tokens, int32_t n_q_heads
     if (n_tokens >= limit || n_tokens * n_q_heads >= limit) return RETOPK_ERR_UNSUPPORTED;
     if (max_len > rows) max_len = rows;
     if (window > rows) window = 0;
-    *out = attend_plan(n_tokens, n_q_heads, c.n_kv_heads, c.head_dim, max_len, window, kAttendSlots);
+    *out = attend_plan(n_tokens, n_q_heads, c.n_kv_heads, c.head_dim, max_len, window,
+                       attend_slots(c.format, c.head_dim), c.format == RETOPK_PAGES_F32 ? kAttendDirectF32 : kAttendDirect);
     return out->waves < limit ? RETOPK_OK : RETOPK_ERR_UNSUPPORTED;
 }
 
@@ -1051,7 +1091,7 @@ retopk_status paged_attention(const retopk_pages *c, int32_t dtype, int64_t n_to
     a.group = n_q_heads / c->n_kv_heads;
     a.max_len = (int32_t)(max_len < rows ? max_len : rows);
     a.window = window <= rows ? (int32_t)window : 0;
-    a.chunks = (int32_t)p.chunks;
+    a.chunks = p.split == ATTEND_DIRECT ? kAttendWaves : (int32_t)p.chunks;
     a.scale2 = (float)(1.44269504088896340736 / __builtin_sqrt((double)d));
     a.out = out;
     a.lse = lse;

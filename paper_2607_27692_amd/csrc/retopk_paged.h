@@ -28,15 +28,23 @@ PagesArgs pages_args(const retopk_pages &c);
 // strides not negative; for a tensor that is written, no two rows on each other.
 bool rows_ok(const retopk_rows &x, int64_t tokens, int64_t heads, int d, int es, bool written);
 
-// The number of the row that holds position p >= 0 of sequence s and KV head g, or -1.
-__device__ __forceinline__ int32_t row_of(const PagesArgs &c, int32_t s, int32_t p, int g)
+// The page of position p of sequence s, -1 for none; and the number of the row that holds it on
+// that page for KV head g, or -1.
+__device__ __forceinline__ int32_t page_of(const PagesArgs &c, int32_t s, int32_t p)
 {
     if (s < 0 || s >= c.n_seqs || p < 0) return -1;
     const uint32_t at = divide((uint32_t)p, c.by_page);
-    if (at >= (uint32_t)c.table_width) return -1;
-    const int32_t page = c.table[(int64_t)s * c.table_width + at];
+    return at < (uint32_t)c.table_width ? c.table[(int64_t)s * c.table_width + at] : -1;
+}
+__device__ __forceinline__ int32_t row_on(const PagesArgs &c, int32_t page, int32_t p, int g)
+{
     if (page < 0 || page >= c.n_pages) return -1;
+    const uint32_t at = divide((uint32_t)p, c.by_page);
     return (page * c.n_kv_heads + g) * c.page_size + (p - (int32_t)at * c.page_size);
+}
+__device__ __forceinline__ int32_t row_of(const PagesArgs &c, int32_t s, int32_t p, int g)
+{
+    return row_on(c, page_of(c, s, p), p, g);
 }
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));

@@ -32,8 +32,11 @@ constexpr uint32_t divide(uint32_t x, Divisor d)
 // each of which works alone.  A token's positions count from its first attended one rounded
 // down to a tile.  The lengths are on the device, the host knows only max_len, so there are
 // three splits:
-//   DIRECT    one wave a group: no group has more than kAttendDirect tiles, and the wave
-//             writes the output itself.
+//   DIRECT    one block a group: no group has more than a few tiles (kAttendDirect; twice and more
+//             where the groups alone fill the chip), and the block's waves join their results
+//             and write the output themselves.  One launch: 500 positions of 4 groups take 9.7 us
+//             from 4-bit pages and 12.7 in BALANCED's two, 1000 take 14.3 and 12.8; 2000 of
+//             1024 groups 43 and 52.
 //   BALANCED  the tiles of all groups in one row, token after token, cut into equal parts on
 //             the device, one a wave, so that ragged lengths leave no wave idle; a part may
 //             span several groups and a group several parts.  At most kAttendTokens tokens,
@@ -44,10 +47,12 @@ constexpr uint32_t divide(uint32_t x, Divisor d)
 // part of a wave begins a new group, each part of a group a new wave).  Where all waves of a
 // block work on one group they join their results under the number of the first.
 constexpr int kAttendTile = 32;       // positions of a tile
-constexpr int kAttendDirect = 8;      // tiles
+constexpr int kAttendDirect = 24;     // tiles
+constexpr int kAttendDirectF32 = 8;   // of f32 pages, whose tiles take three times as long
+constexpr int kAttendDirectFull = 64; // where there is a wave for every slot
 constexpr int kAttendPart = 2;        // fewest tiles of a BALANCED wave
 constexpr int kAttendWaves = 4;       // of a block
-constexpr int kAttendTokens = 256;
+constexpr int kAttendTokens = 1024;
 constexpr int kAttendChunk = 512;     // rows
 
 enum AttendSplit : int { ATTEND_DIRECT = 0, ATTEND_BALANCED = 1, ATTEND_CHUNKED = 2 };
@@ -60,15 +65,15 @@ struct AttendPlan {
     int64_t workspace;         // bytes
 };
 
-// slots: the waves that run at once.
+// slots: the waves that run at once; direct: the tiles of a DIRECT group.
 inline AttendPlan attend_plan(int64_t tokens, int64_t n_q_heads, int64_t n_kv_heads, int d, int64_t max_len,
-                              int64_t window, int64_t slots)
+                              int64_t window, int64_t slots, int direct)
 {
-    AttendPlan p = {ATTEND_DIRECT, tokens * n_kv_heads, 1, 0, 0, 0};
+    AttendPlan p = {ATTEND_DIRECT, tokens * n_kv_heads * kAttendWaves, 1, 0, 0, 0};
     // a window's first position may lie kAttendTile - 1 past the tile it begins in
     const int64_t span = window > 0 && window + kAttendTile - 1 < max_len ? window + kAttendTile - 1 : max_len;
     const int64_t groups = tokens * n_kv_heads, tiles = ceil_div(span, kAttendTile);
-    if (tiles <= kAttendDirect) return p;
+    if (tiles <= (groups * kAttendWaves >= slots ? kAttendDirectFull : direct)) return p;
     if (tokens <= kAttendTokens && groups * tiles < ((int64_t)1 << 31)) {
         p.split = ATTEND_BALANCED;
         const int64_t most = ceil_div(groups * tiles, kAttendPart);

@@ -248,10 +248,10 @@ int main()
         }
     }
     for (int64_t len = 1; len < ((int64_t)1 << 31); len = len < 600 ? len + 1 : len + len / 3 + 11)
-        for (int64_t tokens : {1, 2, 7, 32, 255, 256, 257, 4096})
+        for (int64_t tokens : {1, 2, 7, 32, 1023, 1024, 1025, 4096})
             for (int64_t hkv : {1, 4, 8, 40})
                 for (int64_t w : {0, 1, 31, 32, 33, 4096, 1 << 30}) {
-                    const AttendPlan p = attend_plan(tokens, hkv * 4, hkv, 128, len, w, 512);
+                    const AttendPlan p = attend_plan(tokens, hkv * 4, hkv, 128, len, w, 512, kAttendDirect);
                     // tiles of a token whose window begins as late in its tile as it can
                     int64_t worst = ceil_div(len, kAttendTile);
                     if (w > 0 && w < len) {
@@ -261,7 +261,7 @@ int main()
                             worst = n > worst ? n : worst;
                         }
                     }
-                    if (p.split == ATTEND_DIRECT && (worst > kAttendDirect || p.waves != tokens * hkv || p.workspace))
+                    if (p.split == ATTEND_DIRECT && (worst > (tokens * hkv * kAttendWaves >= 512 ? kAttendDirectFull : kAttendDirect) || p.waves != tokens * hkv * kAttendWaves || p.workspace))
                         return bad("direct", len, w);
                     if (p.split == ATTEND_BALANCED &&
                         (p.waves < 1 || p.waves > 512 || tokens > kAttendTokens || p.parts != p.waves + tokens * hkv))
@@ -278,7 +278,7 @@ int main()
     uint32_t seed = 1;
     auto rnd = [&](uint32_t n) { seed = seed * 1664525u + 1013904223u; return (seed >> 8) % n; };
     for (int round = 0; round < 4000; ++round) {
-        const int tokens = 1 + rnd(round % 7 ? 12 : 256), hkv = 1 + rnd(9), top = 1 + rnd(round % 3 ? 40 : 5000);
+        const int tokens = 1 + rnd(round % 7 ? 12 : 1024), hkv = 1 + rnd(9), top = 1 + rnd(round % 3 ? 40 : 5000);
         std::vector<int> tiles(tokens), ends(tokens);
         int all = 0, most = 0;
         for (int t = 0; t < tokens; ++t) {
@@ -286,7 +286,7 @@ int main()
             most = tiles[t] > most ? tiles[t] : most;
             ends[t] = all += tiles[t] * hkv;
         }
-        const AttendPlan p = attend_plan(tokens, hkv, hkv, 64, (int64_t)(most < 9 ? 9 : most) * kAttendTile, 0, 1 + rnd(512));
+        const AttendPlan p = attend_plan(tokens, hkv, hkv, 64, (int64_t)(most <= kAttendDirectFull ? kAttendDirectFull + 1 : most) * kAttendTile, 0, 1 + rnd(512), kAttendDirect);
         if (p.split != ATTEND_BALANCED) return bad("split", tokens, p.split);
         const int per = (int)attend_part(all, (uint32_t)p.waves);
         if ((int64_t)per * p.waves < all) return bad("part", per, all);
