@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
         auto load = [&](Oct<T> (&x)[U], const char *from, const int32_t (&r)[U]) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                x[u].load((const T *)from + (uint64_t)(uint32_t)max(r[u], 0) * D + e0);
+                x[u].load_once((const T *)from + (uint64_t)(uint32_t)max(r[u], 0) * D + e0);
         };
         if (n_it > 0) {
             look(0);
@@ -411,7 +411,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
             for (int u = 0; u < 2; ++u) {
                 const u32x4_t *p = (const u32x4_t *)(a.c.k + (uint64_t)s_row[wave][it & 1][16 * u + col] * (2 * D));
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) kv[u][ks] = p[ks * 4 + kq];
+                for (int ks = 0; ks < KS; ++ks) kv[u][ks] = once(p + ks * 4 + kq);
             }
         };
         auto load_v = [&](int it) {
@@ -422,13 +422,13 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
                 for (int i = 0; i < 4; ++i) {
                     const char *p = a.c.v + (uint64_t)r[i] * (2 * D) + col * (D / 8);
                     if constexpr (VD == 4) {
-                        const u32x4_t x = *(const u32x4_t *)p;
+                        const u32x4_t x = once((const u32x4_t *)p);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) vv[4 * u + i][e] = x[e];
                     } else {
-                        const uint2 x = *(const uint2 *)p;
-                        vv[4 * u + i][0] = x.x;
-                        vv[4 * u + i][1] = x.y;
+                        const u32x2_t x = once((const u32x2_t *)p);
+                        vv[4 * u + i][0] = x[0];
+                        vv[4 * u + i][1] = x[1];
                     }
                 }
             }
@@ -688,11 +688,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
         for (int u = 0; u < 2; ++u) {
             const char *p = a.c.k + (int64_t)h[u].row * (D / 2);
             if constexpr (KD == 4) {
-                kc[u] = *(const u32x4_t *)(p + k_off);
+                kc[u] = once((const u32x4_t *)(p + k_off));
             } else {
-                const uint2 x = *(const uint2 *)(p + k_off);
-                kc[u][0] = x.x;
-                kc[u][1] = x.y;
+                const u32x2_t x = once((const u32x2_t *)(p + k_off));
+                kc[u][0] = x[0];
+                kc[u][1] = x[1];
             }
         }
     };
@@ -717,8 +717,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
             const char *p = a.c.v + (int64_t)h[u].row * (D / 2);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if constexpr (D == 128) vc[4 * u + i] = *(const uint32_t *)(p + v_off + i * (D / 2));
-                else vc[4 * u + i] = *(const uint16_t *)(p + v_off + i * (D / 2));
+                if constexpr (D == 128) vc[4 * u + i] = once((const uint32_t *)(p + v_off + i * (D / 2)));
+                else vc[4 * u + i] = once((const uint16_t *)(p + v_off + i * (D / 2)));
             }
         }
     };

@@ -312,7 +312,7 @@ __device__ __forceinline__ void quantise4(const float (&x)[8], uint32_t &codes, 
     codes = w[0] | (w[1] << 16);
 }
 
-template <int FMT, int D>
+template <int FMT, int D, bool STREAM>
 __device__ __forceinline__ void store_row(const PagesArgs &c, bool key, int32_t row, int e0, const float (&x)[8])
 {
     if constexpr (FMT == RETOPK_PAGES_Q4) {
@@ -321,17 +321,17 @@ __device__ __forceinline__ void store_row(const PagesArgs &c, bool key, int32_t 
         if (row < 0) return;
         char *base = key ? c.k : c.v;
         uint32_t *pars = key ? c.k_par : c.v_par;
-        *(uint32_t *)(base + (int64_t)row * (D / 2) + e0 / 2) = codes;
+        put<STREAM>((uint32_t *)(base + (int64_t)row * (D / 2) + e0 / 2), codes);
         if (e0 % kGroup4 == 0) pars[(int64_t)row * (D / kGroup4) + e0 / kGroup4] = par;
     } else if constexpr (FMT == RETOPK_PAGES_BF16) {
-        if (row >= 0) Oct<uint16_t>::store((uint16_t *)(key ? c.k : c.v) + (int64_t)row * D + e0, x);
+        if (row >= 0) Oct<uint16_t>::store<STREAM>((uint16_t *)(key ? c.k : c.v) + (int64_t)row * D + e0, x);
     } else {
-        if (row >= 0) Oct<float>::store((float *)(key ? c.k : c.v) + (int64_t)row * D + e0, x);
+        if (row >= 0) Oct<float>::store<STREAM>((float *)(key ? c.k : c.v) + (int64_t)row * D + e0, x);
     }
 }
 
 // paged_append.  The heads a block walks over: queries, then keys, then values.
-template <typename T, int D, int FMT>
+template <typename T, int D, int FMT, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void k_append(PagesArgs c, retopk_rope r, int rotate, Rows<T> k, Rows<T> v,
                                                         Rows<T> q, Rows<T> q_out, const int32_t *seq,
                                                         const int32_t *pos, int64_t n, int n_q, int per_block)
@@ -365,13 +365,13 @@ __global__ __launch_bounds__(kRowThreads) void k_append(PagesArgs c, retopk_rope
                   } else {
                       const bool key = h < n_q + c.n_kv_heads;
                       const int g = h - n_q - (key ? 0 : c.n_kv_heads);
-                      store_row<FMT, D>(c, key, row0 < 0 ? -1 : row0 + g * c.page_size, e0, x);
+                      store_row<FMT, D, STREAM>(c, key, row0 < 0 ? -1 : row0 + g * c.page_size, e0, x);
                   }
               });
 }
 
 // paged_gather.
-template <typename T, int D, int FMT>
+template <typename T, int D, int FMT, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void k_gather(PagesArgs c, Rows<T> k, Rows<T> v, const int32_t *seq,
                                                         const int32_t *pos, int64_t n, int per_block)
 {
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(kRowThreads) void k_gather(PagesArgs c, Rows<T> k, 
             o.load((const float *)(key ? c.k : c.v) + row * D + e0);
             o.get(x);
         }
-        Oct<T>::store(to.at(t, g) + e0, x);
+        Oct<T>::template store<STREAM>(to.at(t, g) + e0, x);
     }
 }
 
@@ -422,10 +422,15 @@ bool row_grid(int64_t n, int d, int64_t heads, RowGrid *out)
     return true;
 }
 
+// Rows that later steps read, not the next kernel, go past the caches once they are more than
+// the L2s hold together.  What the next kernel reads does not (rotated queries, where a reader
+// right after takes 1 to 4 % longer in all than with plain stores).
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
+
 retopk_status launched() { return hipGetLastError() == hipSuccess ? RETOPK_OK : RETOPK_ERR_HIP; }
 
 template <typename T, int D>
-void launch_append(int format, const RowGrid &g, hipStream_t s, const PagesArgs &c, const retopk_rope &r, int rotate,
+void launch_append(int format, bool stream, const RowGrid &g, hipStream_t s, const PagesArgs &c, const retopk_rope &r, int rotate,
                    const retopk_rows &k, const retopk_rows &v, const retopk_rows &q, const retopk_rows &q_out,
                    const int32_t *seq, const int32_t *pos, int64_t n, int n_q)
 {
@@ -434,12 +439,12 @@ void launch_append(int format, const RowGrid &g, hipStream_t s, const PagesArgs 
                            rows_of<T>(q), rows_of<T>(q_out), seq, pos, n, n_q, g.per_block);
     };
     constexpr int own = sizeof(T) == 2 ? RETOPK_PAGES_BF16 : RETOPK_PAGES_F32;
-    if (format == RETOPK_PAGES_Q4) go(k_append<T, D, RETOPK_PAGES_Q4>);
-    else go(k_append<T, D, own>);
+    if (format == RETOPK_PAGES_Q4) stream ? go(k_append<T, D, RETOPK_PAGES_Q4, true>) : go(k_append<T, D, RETOPK_PAGES_Q4, false>);
+    else stream ? go(k_append<T, D, own, true>) : go(k_append<T, D, own, false>);
 }
 
 template <typename T, int D>
-void launch_gather(int format, const RowGrid &g, hipStream_t s, const PagesArgs &c, const retopk_rows &k,
+void launch_gather(int format, bool stream, const RowGrid &g, hipStream_t s, const PagesArgs &c, const retopk_rows &k,
                    const retopk_rows &v, const int32_t *seq, const int32_t *pos, int64_t n)
 {
     auto go = [&](auto kernel) {
@@ -447,8 +452,8 @@ void launch_gather(int format, const RowGrid &g, hipStream_t s, const PagesArgs 
                            g.per_block);
     };
     constexpr int own = sizeof(T) == 2 ? RETOPK_PAGES_BF16 : RETOPK_PAGES_F32;
-    if (format == RETOPK_PAGES_Q4) go(k_gather<T, D, RETOPK_PAGES_Q4>);
-    else go(k_gather<T, D, own>);
+    if (format == RETOPK_PAGES_Q4) stream ? go(k_gather<T, D, RETOPK_PAGES_Q4, true>) : go(k_gather<T, D, RETOPK_PAGES_Q4, false>);
+    else stream ? go(k_gather<T, D, own, true>) : go(k_gather<T, D, own, false>);
 }
 
 // Runs f with the element type of dtype and the head dimension as types.
@@ -568,10 +573,12 @@ retopk_status paged_append(const retopk_pages *c, const retopk_rope *r, int32_t 
     }
     RowGrid g;
     if (!row_grid(n_tokens, d, (int64_t)n_q_heads + 2 * (int64_t)c->n_kv_heads, &g)) return RETOPK_ERR_UNSUPPORTED;
+    const int64_t row = c->format == RETOPK_PAGES_Q4 ? d / 2 : d * es;
+    const bool past = 2 * n_tokens * c->n_kv_heads * row > kStreamBytes;
     const PagesArgs a = pages_args(*c);
     const retopk_rope none = {}, &rope = r ? *r : none;
     by_type(dtype, d, [&](auto zero, auto dim) {
-        launch_append<decltype(zero), decltype(dim)::value>(c->format, g, (hipStream_t)stream, a, rope, r ? 1 : 0, k,
+        launch_append<decltype(zero), decltype(dim)::value>(c->format, past, g, (hipStream_t)stream, a, rope, r ? 1 : 0, k,
                                                             v, q, q_out, seq, pos, n_tokens, n_q_heads);
     });
     return launched();
@@ -591,9 +598,10 @@ retopk_status paged_gather(const retopk_pages *c, int32_t dtype, int64_t n_token
         return RETOPK_ERR_ARG;
     RowGrid g;
     if (!row_grid(n_tokens, d, 2 * (int64_t)c->n_kv_heads, &g)) return RETOPK_ERR_UNSUPPORTED;
+    const bool past = 2 * n_tokens * c->n_kv_heads * d * es > kStreamBytes;
     const PagesArgs a = pages_args(*c);
     by_type(dtype, d, [&](auto zero, auto dim) {
-        launch_gather<decltype(zero), decltype(dim)::value>(c->format, g, (hipStream_t)stream, a, k, v, seq, pos,
+        launch_gather<decltype(zero), decltype(dim)::value>(c->format, past, g, (hipStream_t)stream, a, k, v, seq, pos,
                                                             n_tokens);
     });
     return launched();
