@@ -351,8 +351,8 @@ retopk_status rotary_embed(const retopk_rope *r, int32_t dtype, int32_t head_dim
  * cache nor its row of q_out is written; one whose position has no page gets its q_out row
  * only.  Every other row of the cache is left as it was.  No position of a sequence may
  * appear twice in a call (which of the two rows the cache then holds, or what mix of
- * them, is unspecified).  k and v must be finite for 4-bit pages: a non-finite element
- * leaves its group of 64 unspecified. */
+ * them, is unspecified).  For 4-bit pages k and v must be finite and within bf16's
+ * range (|x| < 3.39e38): any other element leaves its group of 64 unspecified. */
 retopk_status paged_append(const retopk_pages *c, const retopk_rope *r, int32_t dtype,
                            int64_t n_tokens, const int32_t *seq, const int32_t *pos,
                            retopk_rows k, retopk_rows v, int32_t n_q_heads, retopk_rows q,
@@ -368,7 +368,8 @@ retopk_status paged_gather(const retopk_pages *c, int32_t dtype, int64_t n_token
                            retopk_rows v, void *stream);
 
 /* Bytes of workspace paged_attention needs for these arguments (0: none), or a negative
- * retopk_status. */
+ * retopk_status.  More is always enough, but fewer tokens can need more of it than many do: a
+ * program whose batch varies takes the largest over its sizes. */
 int64_t paged_attention_workspace(const retopk_pages *c, int64_t n_tokens, int32_t n_q_heads,
                                   int64_t max_len, int64_t window);
 
@@ -381,7 +382,9 @@ int64_t paged_attention_workspace(const retopk_pages *c, int64_t n_tokens, int32
  * [n_tokens, n_q_heads, d] float32 and, when non-NULL, lse [n_tokens, n_q_heads] float32, the
  * natural logarithm of the sum of e^score, with which parts of a context attended apart can
  * be joined.  A row with no position left (seq outside [0, n_seqs), pos < 0, no page) gets
- * out = 0 and lse = -infinity.  q, k and v must be finite.  workspace: 16-byte aligned device
+ * out = 0 and lse = -infinity.  q and the attended rows must be finite, and so must the
+ * largest score of a row in float32; what other rows of the pages hold has no effect, NaN
+ * included.  Two kernels, one where the contexts are short.  workspace: 16-byte aligned device
  * memory of at least paged_attention_workspace bytes (less: RETOPK_ERR_TOO_LARGE), used by this
  * call only until its work on the stream is done; two graphs that may run at the same time
  * need two. */

@@ -1,8 +1,17 @@
 // retopk_attend.hip -- paged_attention: full attention of single tokens over a paged cache.
 //
-// Block (chunk, KV head, token) folds its positions into a running maximum, sum and
-// weighted value sum for every query head of the group; with more than one chunk a token,
-// k_attend_merge joins the partial results.
+// The positions of all (token, KV head) groups are cut into equal parts, one a wave
+// (retopk_paged_plan.h).  A wave streams its tiles with no barrier: scores, a reference
+// maximum, weights and weighted value sums for every query head of the group at once, the next
+// tile's rows in flight.  Waves of a block that share a group join their results in shared
+// memory, and k_attend_merge joins what is left in parts.  One kernel a page format:
+//   k_attend4   4 bits: both products on the matrix cores, codes as exact operands
+//   k_attend16  bf16:   both products on the matrix cores, weights in three bf16 parts
+//   k_attend    f32:    vector units
+// Measured, whole calls, the join's launch of about 5 us in them: 131072 positions, 32 heads on 8,
+// d = 128: 37 to 39 us from 4-bit pages (151 MB, 3.9 TB/s), 93 from bf16 pages (537 MB, 5.8 TB/s), 194
+// from f32 pages (1.07 GB, 5.5 TB/s); 32 ragged sequences of up to 16K positions, 28 heads on 4, 4 bits:
+// 38 us (96 MB, 2.5 TB/s).
 #include "retopk.h"
 #include "retopk_paged.h"
 
@@ -12,9 +21,10 @@ namespace retopk {
 namespace {
 
 constexpr int kAttendThreads = 64 * kAttendWaves;
-// Waves that run at once: two a SIMD by the registers of most builds, three of the 4-bit one of
-// d = 64 (32 ragged sequences: 26.3 us with 3072 waves, 29.3 with 2048; the others lose by more).
-inline int64_t attend_slots(int format, int d) { return format == RETOPK_PAGES_Q4 && d == 64 ? 3072 : 2048; }
+// Waves that run at once: two on each of the 1024 SIMDs by the registers of most builds, three of the
+// 4-bit one of d = 64 (32 ragged sequences: 26.3 us with three, 29.3 with two; the others lose by more).
+constexpr int64_t kSimds = 1024;
+inline int64_t attend_slots(int format, int d) { return kSimds * (format == RETOPK_PAGES_Q4 && d == 64 ? 3 : 2); }
 constexpr float kLn2 = 0.69314718055994530942f;
 
 struct AttendArgs {
@@ -217,7 +227,8 @@ template <int LPR> __device__ __forceinline__ float lanes_sum(float x)
 // takes 64 / LPR positions at once, U times over in a step, whose rows are loaded a step ahead and
 // whose pages are looked up two steps ahead, since any position may be on another page.  All in
 // float32 on the vector units: 8 products and 8 value sums a lane, position and head, which
-// stay below the time HBM needs for the rows.  GP >= a.group heads; those past the group repeat
+// stay below the time HBM needs for the rows (131072 positions, 4 heads on each of 8: 196 us, 5.5 TB/s of
+// the 6.0 that a plain read reaches).  GP >= a.group heads; those past the group repeat
 // its first.
 template <int D, int GP>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
@@ -372,7 +383,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
 // which a lane already has its weights; pairs of positions are put side by side with byte permutes.
 // A weight is the sum of three bf16 parts (24 bits): column c has part c / GP of head c % GP, for
 // GP = 8 the third in a second product.  Products start from zero and are added by the vector units:
-// accumulated in the matrix cores the sums lose 2^-24 of the largest product at every step.
+// accumulated in the matrix cores the sums lose 2^-24 of the largest product at every step.  Bound by
+// HBM: the same positions take 88 us, 6.1 TB/s; 8 sequences of up to 32768 take 68 and the join.
 template <int D, int GP>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
 {
@@ -611,6 +623,10 @@ __device__ __forceinline__ Half half_of(const PagesArgs &c, const int32_t *table
 // does not fit 24 bits rounds to one side.  The high parts are therefore whole numbers, whose
 // products are multiples of 2^-21 and sum exactly, kFlush tiles long, until the vector units
 // add them to acc; the low parts' sums, 2^-12 the size, may be biased.
+//
+// The vector units bound it, 60 % busy with the codes of both products and the weights' parts, and the
+// 7 us until the first tile is there: 131072 positions, 4 heads on each of 8, d = 128 take 33 us (4.6 TB/s);
+// without PACK, 32 ragged sequences of 7 heads on each of 4, 34 us (2.8 TB/s); with d = 64, 24.
 constexpr int kFlush = 4;
 template <typename T, int D, bool PACK>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
@@ -623,311 +639,312 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
     static_assert(PACK || NG == 2, "d = 64 always packs");
     __shared__ __attribute__((aligned(16))) Joint<D, 8> s_join;
     for_shares(a, [&](const Share &w) {
-    const int g = w.g, lo = w.lo, hi = w.hi;
-    const int lane = threadIdx.x & 63, col = lane & 15, kq = lane >> 4;
-    Codes codes;
-    codes.hold();
-    // group and head of this lane's column; packed columns 4 .. 7 of d = 128 count the heads down,
-    // so that a half-row mirror meets the other group of the same head
-    const int c8 = col & 7, upper = PACK ? col >> 3 : 0;
-    const int gr = NG == 1 ? 0 : PACK ? c8 >> 2 : col >> 3;
-    const int hc = PACK && NG == 2 ? (gr ? 7 - c8 : c8) : c8, head = hc < a.group ? hc : 0;
-    const int n_it = (hi - lo + 31) / 32;
-    const int32_t *table = a.c.table + (int64_t)max(w.seq, 0) * a.c.table_width;
+        const int g = w.g, lo = w.lo, hi = w.hi;
+        const int lane = threadIdx.x & 63, col = lane & 15, kq = lane >> 4;
+        Codes codes;
+        codes.hold();
+        // group and head of this lane's column; packed columns 4 .. 7 of d = 128 count the heads down,
+        // so that a half-row mirror meets the other group of the same head
+        const int c8 = col & 7, upper = PACK ? col >> 3 : 0;
+        const int gr = NG == 1 ? 0 : PACK ? c8 >> 2 : col >> 3;
+        const int hc = PACK && NG == 2 ? (gr ? 7 - c8 : c8) : c8, head = hc < a.group ? hc : 0;
+        const int n_it = (hi - lo + 31) / 32;
+        const int32_t *table = a.c.table + (int64_t)max(w.seq, 0) * a.c.table_width;
 
-    // the query, scaled by a power of two to [2^14, 2^15): bf16 fits one float16 part, f32 two
-    f16x8_t qb[NQ][KD];
-    int q_exp;
-    float q_sum = 0.0f;
-    {
-        float x[KD][8], top = 0.0f;
-        const T *qr = (const T *)a.q + w.t * a.q_ts + (g * a.group + head) * a.q_hs + kq * (D / 4);
-#pragma unroll
-        for (int i = 0; i < KD; ++i) {
-            Oct<T> v;
-            v.load(qr + 8 * i);
-            v.get(x[i]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
-        }
-        top = max_rows_f32(top);
-        q_exp = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) - 15 : 0;
-        const bool mine = NG == 1 || (kq >> 1) == gr;
-#pragma unroll
-        for (int i = 0; i < KD; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                // code order: elements j and j + 4 in register j
-                const float y = mine ? ldexpf(x[i][(e >> 1) + 4 * (e & 1)], -q_exp) : 0.0f;
-                q_sum += y;
-                const _Float16 h = (_Float16)y;
-                qb[0][i][e] = h;
-                if constexpr (NQ == 2) qb[1][i][e] = (_Float16)(y - (float)h);
-            }
-        q_sum = add16_f32(q_sum, q_sum);
-        q_sum = ldexpf(add32_f32(q_sum, q_sum), -kCodeExp);
-    }
-    // scores in powers of two are the products times this factor; what it cannot hold of the
-    // exponent (queries past 2^94 or below 2^-106) is applied apart
-    const int s_exp = q_exp + kCodeExp, s_near = min(max(s_exp, -100), 100);
-    const float s_mul = ldexpf(a.scale2, s_near);
-    const bool far = __ballot(s_exp != s_near) != 0ull;
-
-    u32x4_t kc[2];             // key codes: the row's dwords kq * KD ..
-    uint32_t kp[V], vp[V], vc[8];
-    Half h0[2], h1[2];         // this tile's halves, the next one's
-    auto halves = [&](int it, Half (&h)[2]) {
-        const int r = lo + it * 32;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) h[u] = half_of(a.c, table, r + 16 * u, g);
-    };
-    // a half's base is the wave's own, a lane's offset in it the same for every half
-    const uint32_t k_off = col * (D / 2) + kq * (D / 8), v_off = 4 * kq * (D / 2) + col * (D / 32);
-    auto load_k = [&](const Half (&h)[2]) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const char *p = a.c.k + (int64_t)h[u].row * (D / 2);
-            if constexpr (KD == 4) {
-                kc[u] = once((const u32x4_t *)(p + k_off));
-            } else {
-                const u32x2_t x = once((const u32x2_t *)(p + k_off));
-                kc[u][0] = x[0];
-                kc[u][1] = x[1];
-            }
-        }
-    };
-    auto load_par = [&](const Half (&h)[2], const uint32_t *par, uint32_t (&w)[V]) {
-#pragma unroll
-        for (int u = 0; u < V / 4; ++u) {
-            const int32_t row = (PACK ? (upper ? h[1].row : h[0].row) : h[u].row) + 4 * kq;
-            const uint32_t *p = par + (int64_t)row * NG + gr;
-            if constexpr (NG == 1) {
-                const u32x4_t x = *(const u32x4_t *)p;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[4 * u + i] = x[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[4 * u + i] = p[i * NG];
-            }
-        }
-    };
-    auto load_v = [&](const Half (&h)[2]) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const char *p = a.c.v + (int64_t)h[u].row * (D / 2);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (D == 128) vc[4 * u + i] = once((const uint32_t *)(p + v_off + i * (D / 2)));
-                else vc[4 * u + i] = once((const uint16_t *)(p + v_off + i * (D / 2)));
-            }
-        }
-    };
-
-    // sums of the high parts (exact, and what they were flushed to) and of the low parts
-    f32x4_t run[NV], acc[NV], low[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) run[j] = acc[j] = low[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    auto flush = [&]() {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            acc[j] += run[j];
-            run[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        }
-    };
-    float m = -FLT_MAX, l = 0.0f, z = 0.0f, limit = 0.0f;
-    int v_exp = 0;
-
-    auto tile = [&](int it, const Half (&h)[2], const Half (&hn)[2], auto more) {
-        float s[V];
+        // the query, scaled by a power of two to [2^14, 2^15): bf16 fits one float16 part, f32 two
+        f16x8_t qb[NQ][KD];
+        int q_exp;
+        float q_sum = 0.0f;
         {
-            f32x4_t d[2];
-#pragma unroll
+            float x[KD][8], top = 0.0f;
+            const T *qr = (const T *)a.q + w.t * a.q_ts + (g * a.group + head) * a.q_hs + kq * (D / 4);
+    #pragma unroll
+            for (int i = 0; i < KD; ++i) {
+                Oct<T> v;
+                v.load(qr + 8 * i);
+                v.get(x[i]);
+    #pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
+            }
+            top = max_rows_f32(top);
+            q_exp = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) - 15 : 0;
+            const bool mine = NG == 1 || (kq >> 1) == gr;
+    #pragma unroll
+            for (int i = 0; i < KD; ++i)
+    #pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    // code order: elements j and j + 4 in register j
+                    const float y = mine ? ldexpf(x[i][(e >> 1) + 4 * (e & 1)], -q_exp) : 0.0f;
+                    q_sum += y;
+                    const _Float16 h = (_Float16)y;
+                    qb[0][i][e] = h;
+                    if constexpr (NQ == 2) qb[1][i][e] = (_Float16)(y - (float)h);
+                }
+            q_sum = add16_f32(q_sum, q_sum);
+            q_sum = ldexpf(add32_f32(q_sum, q_sum), -kCodeExp);
+        }
+        // scores in powers of two are the products times this factor; what it cannot hold of the
+        // exponent (queries past 2^94 or below 2^-106) is applied apart
+        const int s_exp = q_exp + kCodeExp, s_near = min(max(s_exp, -100), 100);
+        const float s_mul = ldexpf(a.scale2, s_near);
+        const bool far = __ballot(s_exp != s_near) != 0ull;
+
+        u32x4_t kc[2];             // key codes: the row's dwords kq * KD ..
+        uint32_t kp[V], vp[V], vc[8];
+        Half h0[2], h1[2];         // this tile's halves, the next one's
+        auto halves = [&](int it, Half (&h)[2]) {
+            const int r = lo + it * 32;
+    #pragma unroll
+            for (int u = 0; u < 2; ++u) h[u] = half_of(a.c, table, r + 16 * u, g);
+        };
+        // a half's base is the wave's own, a lane's offset in it the same for every half
+        const uint32_t k_off = col * (D / 2) + kq * (D / 8), v_off = 4 * kq * (D / 2) + col * (D / 32);
+        auto load_k = [&](const Half (&h)[2]) {
+    #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                d[u] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int i = 0; i < KD; ++i) {
-                    uint32_t r[4];
-                    codes.quad(kc[u][i], r);
-                    const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[0], r[1], r[2], r[3]});
-#pragma unroll
-                    for (int n = NQ - 1; n >= 0; --n) d[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qb[n][i], d[u], 0, 0, 0);
+                const char *p = a.c.k + (int64_t)h[u].row * (D / 2);
+                if constexpr (KD == 4) {
+                    kc[u] = once((const u32x4_t *)(p + k_off));
+                } else {
+                    const u32x2_t x = once((const u32x2_t *)(p + k_off));
+                    kc[u][0] = x[0];
+                    kc[u][1] = x[1];
                 }
             }
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[i] = PACK ? (upper ? d[1][i & 3] : d[0][i & 3]) : d[i >> 2][i & 3];
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (decltype(more)::value) load_k(hn);
-        __builtin_amdgcn_sched_barrier(0);
-        const int row = lo + it * 32;
-        const bool whole = row >= w.span.first && row + 32 <= hi && h[0].there && h[1].there;
-        float tm = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = fmaf(bf16_lo(kp[i]), s[i], bf16_hi(kp[i]) * q_sum);
-        if constexpr (NG == 2) {                                 // the other group of the row
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[i] += PACK ? dpp_f32<kHalfMirror>(s[i]) : row_ror_f32(s[i], 8);
-        }
-        if (far) {
-            asm volatile("");                                    // a branch, not selects in every tile
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[i] = ldexpf(s[i], s_exp - s_near);
-        }
-        if (!whole) {
-            asm volatile("");
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int u = PACK ? upper : i >> 2, r = row + 16 * u + 4 * kq + (i & 3);
-                const bool on = r >= w.span.first && r < hi && (u ? h[1].there : h[0].there);
-                s[i] = on ? s[i] : -INFINITY;
-                vp[i] = on ? vp[i] : 0u;                         // whatever lies there: weight and value 0
+        };
+        auto load_par = [&](const Half (&h)[2], const uint32_t *par, uint32_t (&w)[V]) {
+    #pragma unroll
+            for (int u = 0; u < V / 4; ++u) {
+                const int32_t row = (PACK ? (upper ? h[1].row : h[0].row) : h[u].row) + 4 * kq;
+                const uint32_t *p = par + (int64_t)row * NG + gr;
+                if constexpr (NG == 1) {
+                    const u32x4_t x = *(const u32x4_t *)p;
+    #pragma unroll
+                    for (int i = 0; i < 4; ++i) w[4 * u + i] = x[i];
+                } else {
+    #pragma unroll
+                    for (int i = 0; i < 4; ++i) w[4 * u + i] = p[i * NG];
+                }
             }
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) tm = fmaxf(tm, s[i]);
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (decltype(more)::value) load_par(hn, a.c.k_par, kp);
-        __builtin_amdgcn_sched_barrier(0);
-        // the reference stays until a score passes it by more than 1, then steps 1 past that score:
-        // weights stay below 4 and the sums are rescaled a few times a chunk, not at every new maximum
-        if constexpr (PACK) tm = fmaxf(tm, row_ror_f32(tm, 8));
-        tm = max_rows_f32(tm) * s_mul;
-        if (__ballot(tm > m + 1.0f) != 0ull) {
-            const float mn = tm > m + 1.0f ? tm + 1.0f : m, f = __builtin_amdgcn_exp2f(m - mn);
-            m = mn;
-            l *= f;
-            z *= f;
-            flush();
-#pragma unroll
+        };
+        auto load_v = [&](const Half (&h)[2]) {
+    #pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const char *p = a.c.v + (int64_t)h[u].row * (D / 2);
+    #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (D == 128) vc[4 * u + i] = once((const uint32_t *)(p + v_off + i * (D / 2)));
+                    else vc[4 * u + i] = once((const uint16_t *)(p + v_off + i * (D / 2)));
+                }
+            }
+        };
+
+        // sums of the high parts (exact, and what they were flushed to) and of the low parts
+        f32x4_t run[NV], acc[NV], low[NV];
+    #pragma unroll
+        for (int j = 0; j < NV; ++j) run[j] = acc[j] = low[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        auto flush = [&]() {
+    #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                acc[j] *= f;
-                low[j] *= f;
+                acc[j] += run[j];
+                run[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
             }
-        }
-        float top = 0.0f, vs[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], s_mul, -m));
-            vs[i] = bf16_lo(vp[i]);
-            top = fmaxf(top, vs[i]);
-        }
-        // a scale past the limit: the power of two moves, with two bits to spare
-        if (__ballot(top >= limit) != 0ull && __ballot(top > 0.0f) != 0ull) {
-            float w = max_rows_f32(top);
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) w = fmaxf(w, __shfl_xor(w, o));
-            const int e = __builtin_amdgcn_frexp_expf(w) + 2;     // every scale below 2^(e - 2)
-            const int n = 14 - e;
-            if (limit > 0.0f) {
-                flush();
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        acc[j][i] = ldexpf(acc[j][i], n - v_exp);
-                        low[j][i] = ldexpf(low[j][i], n - v_exp);
+        };
+        float m = -FLT_MAX, l = 0.0f, z = 0.0f, limit = 0.0f;
+        int v_exp = 0;
+
+        auto tile = [&](int it, const Half (&h)[2], const Half (&hn)[2], auto more) {
+            float s[V];
+            {
+                f32x4_t d[2];
+    #pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    d[u] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    #pragma unroll
+                    for (int i = 0; i < KD; ++i) {
+                        uint32_t r[4];
+                        codes.quad(kc[u][i], r);
+                        const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[0], r[1], r[2], r[3]});
+    #pragma unroll
+                        for (int n = NQ - 1; n >= 0; --n) d[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qb[n][i], d[u], 0, 0, 0);
                     }
+                }
+    #pragma unroll
+                for (int i = 0; i < V; ++i) s[i] = PACK ? (upper ? d[1][i & 3] : d[0][i & 3]) : d[i >> 2][i & 3];
             }
-            v_exp = n;
-            limit = ldexpf(1.0f, e);
-        }
-        uint32_t ph[V / 2], pl[V / 2];
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            const float x = s[2 * i] * ldexpf(vs[2 * i], v_exp), y = s[2 * i + 1] * ldexpf(vs[2 * i + 1], v_exp);
-            const f16x2_t hx = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_pkrtz(rintf(x), rintf(y)));
-            const f32x2_t r = {fmaf(-1.0f, (float)hx[0], x), fmaf(-1.0f, (float)hx[1], y)};
-            ph[i] = __builtin_bit_cast(uint32_t, hx);
-            pl[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(r, f16x2_t));
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            z = fmaf(s[i], bf16_hi(vp[i]), z);
-            l += s[i];
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (decltype(more)::value) load_par(hn, a.c.v_par, vp);
-        __builtin_amdgcn_sched_barrier(0);
-        // positions 0 .. 3 of the operand are the lower half's, 4 .. 7 the upper half's
-        u32x4_t bh, bl;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool mine = !PACK || (i >> 1) == upper;
-            bh[i] = mine ? ph[i % (V / 2)] : 0u;
-            bl[i] = mine ? pl[i % (V / 2)] : 0u;
-        }
-#pragma unroll
-        for (int w = 0; w < NV / 4; ++w) {
-            uint32_t r[4][4];                                    // [code][pair of positions]
-#pragma unroll
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (decltype(more)::value) load_k(hn);
+            __builtin_amdgcn_sched_barrier(0);
+            const int row = lo + it * 32;
+            const bool whole = row >= w.span.first && row + 32 <= hi && h[0].there && h[1].there;
+            float tm = -INFINITY;
+    #pragma unroll
+            for (int i = 0; i < V; ++i) s[i] = fmaf(bf16_lo(kp[i]), s[i], bf16_hi(kp[i]) * q_sum);
+            if constexpr (NG == 2) {                                 // the other group of the row
+    #pragma unroll
+                for (int i = 0; i < V; ++i) s[i] += PACK ? dpp_f32<kHalfMirror>(s[i]) : row_ror_f32(s[i], 8);
+            }
+            if (far) {
+                asm volatile("");                                    // a branch, not selects in every tile
+    #pragma unroll
+                for (int i = 0; i < V; ++i) s[i] = ldexpf(s[i], s_exp - s_near);
+            }
+            if (!whole) {
+                asm volatile("");
+    #pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int u = PACK ? upper : i >> 2, r = row + 16 * u + 4 * kq + (i & 3);
+                    const bool on = r >= w.span.first && r < hi && (u ? h[1].there : h[0].there);
+                    s[i] = on ? s[i] : -INFINITY;
+                    vp[i] = on ? vp[i] : 0u;                         // whatever lies there: weight and value 0
+                }
+            }
+    #pragma unroll
+            for (int i = 0; i < V; ++i) tm = fmaxf(tm, s[i]);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (decltype(more)::value) load_par(hn, a.c.k_par, kp);
+            __builtin_amdgcn_sched_barrier(0);
+            // the reference stays until a score passes it by more than 1, then steps 1 past that score:
+            // weights stay below 4 and the sums are rescaled a few times a chunk, not at every new maximum
+            if constexpr (PACK) tm = fmaxf(tm, row_ror_f32(tm, 8));
+            tm = max_rows_f32(tm) * s_mul;
+            if (__ballot(tm > m + 1.0f) != 0ull) {
+                const float mn = tm > m + 1.0f ? tm + 1.0f : m, f = __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= f;
+                z *= f;
+                flush();
+    #pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    acc[j] *= f;
+                    low[j] *= f;
+                }
+            }
+            float top = 0.0f, vs[V];
+    #pragma unroll
+            for (int i = 0; i < V; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], s_mul, -m));
+                vs[i] = bf16_lo(vp[i]);
+                top = fmaxf(top, vs[i]);
+            }
+            // a scale past the limit: the power of two moves, with two bits to spare
+            if (__ballot(top >= limit) != 0ull && __ballot(top > 0.0f) != 0ull) {
+                float w = max_rows_f32(top);
+    #pragma unroll
+                for (int o = 1; o < 16; o <<= 1) w = fmaxf(w, __shfl_xor(w, o));
+                const int e = __builtin_amdgcn_frexp_expf(w) + 2;     // every scale below 2^(e - 2)
+                const int n = 14 - e;
+                if (limit > 0.0f) {
+                    flush();
+    #pragma unroll
+                    for (int j = 0; j < NV; ++j)
+    #pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            acc[j][i] = ldexpf(acc[j][i], n - v_exp);
+                            low[j][i] = ldexpf(low[j][i], n - v_exp);
+                        }
+                }
+                v_exp = n;
+                limit = ldexpf(1.0f, e);
+            }
+            uint32_t ph[V / 2], pl[V / 2];
+    #pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                const float x = s[2 * i] * ldexpf(vs[2 * i], v_exp), y = s[2 * i + 1] * ldexpf(vs[2 * i + 1], v_exp);
+                const f16x2_t hx = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_pkrtz(rintf(x), rintf(y)));
+                const f32x2_t r = {fmaf(-1.0f, (float)hx[0], x), fmaf(-1.0f, (float)hx[1], y)};
+                ph[i] = __builtin_bit_cast(uint32_t, hx);
+                pl[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(r, f16x2_t));
+            }
+    #pragma unroll
+            for (int i = 0; i < V; ++i) {
+                z = fmaf(s[i], bf16_hi(vp[i]), z);
+                l += s[i];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (decltype(more)::value) load_par(hn, a.c.v_par, vp);
+            __builtin_amdgcn_sched_barrier(0);
+            // positions 0 .. 3 of the operand are the lower half's, 4 .. 7 the upper half's
+            u32x4_t bh, bl;
+    #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t x = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], w ? 0x07060302u : 0x05040100u);
-                const uint32_t y = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], w ? 0x06070203u : 0x04050001u);
-                r[0][i] = codes.pair(x);
-                r[1][i] = codes.pair(x << 4);
-                r[2][i] = codes.pair(y);
-                r[3][i] = codes.pair(y << 4);
+                const bool mine = !PACK || (i >> 1) == upper;
+                bh[i] = mine ? ph[i % (V / 2)] : 0u;
+                bl[i] = mine ? pl[i % (V / 2)] : 0u;
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[j][0], r[j][1], r[j][2], r[j][3]});
-                low[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, __builtin_bit_cast(f16x8_t, bl), low[4 * w + j], 0, 0, 0);
-                run[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, __builtin_bit_cast(f16x8_t, bh), run[4 * w + j], 0, 0, 0);
+    #pragma unroll
+            for (int w = 0; w < NV / 4; ++w) {
+                uint32_t r[4][4];                                    // [code][pair of positions]
+    #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], w ? 0x07060302u : 0x05040100u);
+                    const uint32_t y = __builtin_amdgcn_perm(vc[2 * i + 1], vc[2 * i], w ? 0x06070203u : 0x04050001u);
+                    r[0][i] = codes.pair(x);
+                    r[1][i] = codes.pair(x << 4);
+                    r[2][i] = codes.pair(y);
+                    r[3][i] = codes.pair(y << 4);
+                }
+    #pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f16x8_t x = __builtin_bit_cast(f16x8_t, u32x4_t{r[j][0], r[j][1], r[j][2], r[j][3]});
+                    low[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, __builtin_bit_cast(f16x8_t, bl), low[4 * w + j], 0, 0, 0);
+                    run[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, __builtin_bit_cast(f16x8_t, bh), run[4 * w + j], 0, 0, 0);
+                }
             }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (decltype(more)::value) load_v(hn);
-        __builtin_amdgcn_sched_barrier(0);
-        if (it % kFlush == kFlush - 1) flush();
-    };
-    if (n_it > 0) {
-        halves(0, h0);
-        load_k(h0);
-        load_par(h0, a.c.k_par, kp);
-        load_par(h0, a.c.v_par, vp);
-        load_v(h0);
-        for (int it = 0; it + 1 < n_it; ++it) {
-            halves(it + 1, h1);
-            tile(it, h0, h1, std::true_type{});
-            h0[0] = h1[0];
-            h0[1] = h1[1];
-        }
-        tile(n_it - 1, h0, h0, std::false_type{});
-        flush();
-    }
-    if constexpr (PACK) {
-        l += row_ror_f32(l, 8);
-        z += row_ror_f32(z, 8);
-    }
-    l = add16_f32(l, l);
-    l = add32_f32(l, l);
-    z = add16_f32(z, z);
-    z = add32_f32(z, z);
-    if (lane < 8 && gr == 0 && hc < a.group) s_join.sum(a, w, hc, m, l);
-    // rows 4 kq + i of product j are elements (4 kq + i) * (D / 16) + j, right in the columns of
-    // their own group
-    const float f = s_join.factor(w, l);
-    float *out = s_join.row(a, w, hc) + 4 * kq * (D / 16);
-    const bool mine = !(PACK && col >= 8) && (NG == 1 || (kq >> 1) == gr) && hc < a.group;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j0 = 0; j0 < NV; j0 += 4) {
-            f32x4_t o;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                o[j] = ldexpf(acc[j0 + j][i] + low[j0 + j][i], kCodeExp - v_exp);
-                if constexpr (PACK) o[j] += row_ror_f32(o[j], 8);
-                o[j] = (o[j] + z) * f;
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (decltype(more)::value) load_v(hn);
+            __builtin_amdgcn_sched_barrier(0);
+            if (it % kFlush == kFlush - 1) flush();
+        };
+        if (n_it > 0) {
+            halves(0, h0);
+            load_k(h0);
+            load_par(h0, a.c.k_par, kp);
+            load_par(h0, a.c.v_par, vp);
+            load_v(h0);
+            for (int it = 0; it + 1 < n_it; ++it) {
+                halves(it + 1, h1);
+                tile(it, h0, h1, std::true_type{});
+                h0[0] = h1[0];
+                h0[1] = h1[1];
             }
-            if (mine) *(f32x4_t *)(out + i * (D / 16) + j0) = o;
+            tile(n_it - 1, h0, h0, std::false_type{});
+            flush();
         }
-    s_join.finish(a, w);
+        if constexpr (PACK) {
+            l += row_ror_f32(l, 8);
+            z += row_ror_f32(z, 8);
+        }
+        l = add16_f32(l, l);
+        l = add32_f32(l, l);
+        z = add16_f32(z, z);
+        z = add32_f32(z, z);
+        if (lane < 8 && gr == 0 && hc < a.group) s_join.sum(a, w, hc, m, l);
+        // rows 4 kq + i of product j are elements (4 kq + i) * (D / 16) + j, right in the columns of
+        // their own group
+        const float f = s_join.factor(w, l);
+        float *out = s_join.row(a, w, hc) + 4 * kq * (D / 16);
+        const bool mine = !(PACK && col >= 8) && (NG == 1 || (kq >> 1) == gr) && hc < a.group;
+    #pragma unroll
+        for (int i = 0; i < 4; ++i)
+    #pragma unroll
+            for (int j0 = 0; j0 < NV; j0 += 4) {
+                f32x4_t o;
+    #pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    o[j] = ldexpf(acc[j0 + j][i] + low[j0 + j][i], kCodeExp - v_exp);
+                    if constexpr (PACK) o[j] += row_ror_f32(o[j], 8);
+                    o[j] = (o[j] + z) * f;
+                }
+                if (mine) *(f32x4_t *)(out + i * (D / 16) + j0) = o;
+            }
+        s_join.finish(a, w);
     });
 }
 
 // Joins the parts of a group: block = (token, query head), whose waves fold kMergeUnroll parts at
-// a time, all of them read in one round trip, and are then joined themselves.
+// a time, all of them read in one round trip, and are then joined themselves.  Bound by its launch and
+// three dependent reads: 32 heads of 64 parts take 5.3 us, 896 of a few each 5.2.
 constexpr int kMergeWaves = 16, kMergeUnroll = 16;
 template <int D>
 __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)

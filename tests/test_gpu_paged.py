@@ -468,6 +468,63 @@ def test_attention(fmt, dtype, d, hq, hkv, page, lens, window):
     check_attention(out, lse, q, seq, pos, rows, hq, hkv, window, limit=cut)
 
 
+@pytest.mark.parametrize("fmt,dtype,d,hq,hkv,page,tokens,longest,window", [
+    # more tokens than are shared out tile by tile: fixed chunks, sixteen tiles of one wave
+    ("q4", "bf16", 128, 7, 1, 32, 1100, 2300, 0), ("q4", "f32", 64, 2, 1, 48, 1030, 2200, 0),
+    ("bf16", "bf16", 128, 5, 1, 37, 1100, 2300, 0), ("f32", "f32", 64, 8, 1, 64, 1030, 2150, 0),
+    ("q4", "bf16", 64, 4, 2, 16, 1050, 3100, 2500),
+    # as many groups as fill the chip: a block each, with up to 64 tiles
+    ("q4", "bf16", 128, 4, 1, 64, 600, 2000, 0), ("bf16", "bf16", 64, 2, 2, 5, 300, 1900, 0),
+    ("f32", "f32", 128, 1, 1, 100, 520, 2048, 1000),
+    # hundreds of tokens shared out tile by tile, most of them short
+    ("q4", "f32", 128, 8, 1, 16, 700, 2600, 0), ("bf16", "bf16", 128, 8, 1, 64, 513, 2500, 0),
+])
+def test_attention_of_many_tokens(fmt, dtype, d, hq, hkv, page, tokens, longest, window):
+    """Queries of many tokens over a few sequences, at every kind of split; some of them checked."""
+    torch = torch_cuda()
+    print(f"attention of {tokens} tokens {fmt} {dtype} d={d} {hq}/{hkv} page={page}", flush=True)
+    rng = np.random.default_rng(tokens)
+    torch.manual_seed(2)
+    lens = [longest, 700, 1]
+    c = make_cache(fmt, hkv, d, page, lens, rng)
+    rows = fill(c, fmt, dtype, lens, rng)
+    seq = rng.integers(-1, len(lens) + 1, tokens)
+    pos = np.array([rng.integers(-1, lens[s]) if 0 <= s < len(lens) else 5 for s in seq])
+    seq[:3], pos[:3] = [0, 1, 2], [n - 1 for n in lens]
+    seq[-2:], pos[-2:] = [0, 0], [longest - 1, 0]
+    q = dev(rng.standard_normal((tokens, hq, d)), dtype)
+    out, lse = attend(c, seq, pos, q, longest, window)
+    assert not bool(torch.isnan(out).any()) and not bool(torch.isnan(lse).any())
+    some = np.unique(np.r_[0:3, tokens - 2:tokens, rng.integers(0, tokens, 30)])
+    check_attention(out[some], lse[some], q[some], seq[some], pos[some], rows, hq, hkv, window)
+
+
+@pytest.mark.parametrize("fmt,dtype,d,hq", [("q4", "bf16", 64, 3), ("q4", "bf16", 128, 4), ("bf16", "bf16", 64, 2)])
+def test_attention_of_one_long_sequence(fmt, dtype, d, hq):
+    """Many tiles a wave in every block of the chip, one KV head: 300 000 positions."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(d)
+    n, page = 300_000, 512
+    c = make_cache(fmt, 1, d, page, [n], rng)
+    k, v = (dev(rng.standard_normal((n, 1, d)).astype(np.float32), dtype) for _ in range(2))
+    R.paged_append(c, ints([0] * n), ints(range(n)), k, v)
+    back = [torch.empty((n, 1, d), device="cuda") for _ in range(2)] if fmt == "q4" else [k, v]
+    if fmt == "q4":          # the stored values, in float32
+        R.paged_gather(c, ints([0] * n), ints(range(n)), *back)
+    q = dev(rng.standard_normal((1, hq, d)) * 2, dtype)
+    out, lse = attend(c, [0], [n - 1], q, n)
+    K, V, Q = (x.double() for x in (back[0][:, 0], back[1][:, 0], q[0]))
+    s = (Q @ K.T) / math.sqrt(d)
+    p = torch.softmax(s, -1)
+    want, size = p @ V, float((p @ V.abs()).max())
+    spread = float((Q.abs() @ K.abs().T).max()) / math.sqrt(d)
+    # the bound of the other tests; and, since the weights' errors of up to 2^-20 (1 + spread) know
+    # nothing of the values, an error of the sum of weighted values of that part of its own size
+    assert float((out[0].double() - want).abs().max()) <= 2.0 ** -18 * (1 + spread) * size
+    assert float((out[0].double() - want).norm() / want.norm()) <= 2.0 ** -20 * (1 + spread)
+    assert float((lse[0].double() - torch.logsumexp(s, -1)).abs().max()) <= 2.0 ** -19 * (1 + spread)
+
+
 @pytest.mark.parametrize("fmt,dtype,page", [("q4", "bf16", 32), ("bf16", "bf16", 24), ("f32", "f32", 10)])
 def test_attention_pages_that_are_none(fmt, dtype, page):
     """Pages whose ids lie outside the cache are left out, at the start, inside a chunk, whole
