@@ -421,6 +421,9 @@ class PagedCache:
         self.q4 = k.element_size() == 1
         n, hkv, page, d = k.shape
         if self.q4:
+            import torch
+            if k.dtype != torch.uint8:
+                raise RetopkError(fn, -1, f"k is {k.dtype}: float32, bfloat16 or uint8 expected")
             d *= 2
             if k_par is None or v_par is None:
                 raise RetopkError(fn, -1, "4-bit pages need k_par and v_par")
@@ -454,6 +457,8 @@ class PagedCache:
         """A cache of empty pages; fmt: "f32", "bf16" or "q4".  No sequence has a page yet
         (the table holds -1)."""
         import torch
+        if fmt not in ("f32", "bf16", "q4"):
+            raise RetopkError("retopk_pages", -1, f"format {fmt!r}: f32, bf16 or q4 expected")
         shape, dev = (n_pages, n_kv_heads, page_size), dict(device=device)
         table = torch.full((n_seqs, table_width), -1, dtype=torch.int32, **dev)
         if fmt == "q4":

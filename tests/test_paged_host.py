@@ -359,3 +359,15 @@ def test_binding_refuses_before_the_library():
         R.rotary_embed(R.make_rope(64), z(3, 2, 64), z(3, dtype=torch.int32), z(3, 2, 64))
     with pytest.raises(R.RetopkError):
         R.PagedCache(z(16, 64), z(16, 64), z(1, 2, dtype=torch.int32))
+
+
+def test_cache_formats_are_checked():
+    """Rows of another one-byte type are no codes; formats have three names."""
+    torch = pytest.importorskip("torch")
+    par, table = (torch.zeros(s, dtype=torch.int32) for s in ((2, 1, 16, 1), (1, 2)))
+    for dt in (torch.int8, torch.bool, torch.float8_e4m3fn):
+        k = torch.zeros((2, 1, 16, 32), dtype=dt)
+        with pytest.raises(R.RetopkError, match="uint8"):
+            R.PagedCache(k, k, table, par, par)
+    with pytest.raises(R.RetopkError, match="bf16"):
+        R.PagedCache.allocate("fp8", 2, 1, 16, 64, 1, 2, device="cpu")
