@@ -382,9 +382,9 @@ int64_t paged_attention_workspace(const retopk_pages *c, int64_t n_tokens, int32
  * [n_tokens, n_q_heads, d] float32 and, when non-NULL, lse [n_tokens, n_q_heads] float32, the
  * natural logarithm of the sum of e^score, with which parts of a context attended apart can
  * be joined.  A row with no position left (seq outside [0, n_seqs), pos < 0, no page) gets
- * out = 0 and lse = -infinity.  q and the attended rows must be finite, and so must the
- * largest score of a row in float32; what other rows of the pages hold has no effect, NaN
- * included.  Two kernels, one where the contexts are short.  workspace: 16-byte aligned device
+ * out = 0 and lse = -infinity.  q and the attended rows must be finite, and in float32
+ * so must the largest score of a row and 4 max_len times the largest |v|, which the sums may
+ * reach before they are divided; what other rows of the pages hold has no effect, NaN included.  Two kernels, one where the contexts are short.  workspace: 16-byte aligned device
  * memory of at least paged_attention_workspace bytes (less: RETOPK_ERR_TOO_LARGE), used by this
  * call only until its work on the stream is done; two graphs that may run at the same time
  * need two. */

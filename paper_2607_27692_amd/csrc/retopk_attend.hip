@@ -26,6 +26,10 @@ constexpr int kAttendThreads = 64 * kAttendWaves;
 constexpr int64_t kSimds = 1024;
 inline int64_t attend_slots(int format, int d) { return kSimds * (format == RETOPK_PAGES_Q4 && d == 64 ? 3 : 2); }
 constexpr float kLn2 = 0.69314718055994530942f;
+// A weight is 2^(s * mul - m) in one rounding while the reference m is no larger; past it the rounding
+// of m is no longer small (of 2^31 it is 128: a weight of infinity, or all of them 0), and s * mul is
+// rounded before the difference as m was.
+constexpr float kNearReference = 65536.0f;
 
 struct AttendArgs {
     PagesArgs c;
@@ -449,6 +453,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
 #pragma unroll
         for (int j = 0; j < NV; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         float m = -FLT_MAX, l = 0.0f;
+        bool big = false;                              // a reference past kNearReference
         const float after1 = part >= 1 ? 1.0f : 0.0f, after2 = part >= 2 ? 1.0f : 0.0f;
 
         uint32_t on = 0u, on_next = 0u;
@@ -503,10 +508,17 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
                 l *= f;
 #pragma unroll
                 for (int j = 0; j < NV; ++j) acc[j] *= f;
+                big = __ballot(fabsf(m) > kNearReference) != 0ull;
             }
+            if (big) {
+                asm volatile("");                      // as above
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] *= a.scale2;
+            }
+            const float by = big ? 1.0f : a.scale2;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale2, -m));
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], by, -m));
                 l += s[i];
             }
             // this column's part of the weights; the third one too
@@ -751,6 +763,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
             }
         };
         float m = -FLT_MAX, l = 0.0f, z = 0.0f, limit = 0.0f;
+        bool big = false;                                    // a reference past kNearReference
         int v_exp = 0;
 
         auto tile = [&](int it, const Half (&h)[2], const Half (&hn)[2], auto more) {
@@ -819,11 +832,18 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
                     acc[j] *= f;
                     low[j] *= f;
                 }
+                big = __ballot(fabsf(m) > kNearReference) != 0ull;
             }
+            if (big) {
+                asm volatile("");
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[i] *= s_mul;
+            }
+            const float by = big ? 1.0f : s_mul;
             float top = 0.0f, vs[V];
     #pragma unroll
             for (int i = 0; i < V; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], s_mul, -m));
+                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], by, -m));
                 vs[i] = bf16_lo(vp[i]);
                 top = fmaxf(top, vs[i]);
             }

@@ -525,6 +525,38 @@ def test_attention_of_one_long_sequence(fmt, dtype, d, hq):
     assert float((lse[0].double() - torch.logsumexp(s, -1)).abs().max()) <= 2.0 ** -19 * (1 + spread)
 
 
+@pytest.mark.parametrize("fmt,dtype,d,hq", [
+    ("q4", "bf16", 64, 2), ("q4", "bf16", 128, 4), ("q4", "f32", 128, 7), ("bf16", "bf16", 64, 3),
+    ("bf16", "bf16", 128, 8), ("f32", "f32", 64, 4)])
+@pytest.mark.parametrize("n", [200, 5000])
+def test_attention_of_scores_of_any_size(fmt, dtype, d, hq, n):
+    """Two equal rows whose scores pass all others by far, at sizes up to 2^100: the mean of their
+    values.  A rounded maximum that large is off by more than every exponent of 32 bits."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(n + d + hq)
+    c = make_cache(fmt, 1, d, 16, [n], rng)
+    unit = rng.standard_normal((1, 1, d))
+    for size in (2.0 ** 8, 2.0 ** 18, 2.0 ** 27, 2.0 ** 50):
+        x = rng.standard_normal((n, 1, d)) * 0.01
+        x[[n // 3, n - 2]] = unit
+        k, v = dev(x * size, dtype), dev(rng.standard_normal((n, 1, d)), dtype)
+        R.paged_append(c, ints([0] * n), ints(range(n)), k, v)
+        back = [torch.empty((n, 1, d), device="cuda") for _ in range(2)] if fmt == "q4" else [k, v]
+        if fmt == "q4":
+            R.paged_gather(c, ints([0] * n), ints(range(n)), *back)
+        q = dev(np.repeat(unit, hq, 1) * size * (1 + np.arange(hq) / 8)[:, None], dtype)
+        out, lse = attend(c, [0], [n - 1], q, n)
+        K, V, Q = (y.double() for y in (back[0][:, 0], back[1][:, 0], q[0]))
+        s = (Q @ K.T) / math.sqrt(d)
+        # the others' weights: at least 0.9 of the score's cosine away, e^-1000 at the smallest size
+        assert float((s.max(1).values - s.sort(1).values[:, -3]).min()) > 1000
+        want = (V[n // 3] + V[n - 2]) / 2
+        # weights of 22 bits and more, a few roundings of the sums
+        assert float((out[0].double() - want).abs().max()) <= 2.0 ** -18 * float(V.abs().max())
+        spread = (Q.abs() @ K.abs().T).max(1).values / math.sqrt(d)
+        assert bool(((lse[0].double() - s.max(1).values - math.log(2)).abs() <= 2.0 ** -19 * (1 + spread)).all())
+
+
 @pytest.mark.parametrize("fmt,dtype,page", [("q4", "bf16", 32), ("bf16", "bf16", 24), ("f32", "f32", 10)])
 def test_attention_pages_that_are_none(fmt, dtype, page):
     """Pages whose ids lie outside the cache are left out, at the start, inside a chunk, whole
