@@ -11,7 +11,7 @@
 // Measured, whole calls, the join's launch of about 5 us in them: 131072 positions, 32 heads on 8,
 // d = 128: 37 to 39 us from 4-bit pages (151 MB, 3.9 TB/s), 93 from bf16 pages (537 MB, 5.8 TB/s), 194
 // from f32 pages (1.07 GB, 5.5 TB/s); 32 ragged sequences of up to 16K positions, 28 heads on 4, 4 bits:
-// 38 us (96 MB, 2.5 TB/s).
+// 32 us (96 MB, 3.0 TB/s).
 #include "retopk.h"
 #include "retopk_paged.h"
 
@@ -41,7 +41,7 @@ struct AttendArgs {
     int32_t split, waves, chunks;      // AttendPlan
     float scale2;              // log2(e) / sqrt(d): scores are in powers of two
     float *out, *lse;
-    int32_t *ends;             // BALANCED: [n_tokens] tiles up to and with a token, then a part's tiles
+    int32_t *ends;             // BALANCED: [n_tokens] tiles up to and with a token; a part's tiles; a start's
     float *part_o;             // [parts, group, d]
     float2 *part_ml;           // [parts, group]: maximum (a power of two), sum
 };
@@ -89,6 +89,7 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
     const int worker = blockIdx.x * kAttendWaves + __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool balanced = a.split == ATTEND_BALANCED;
     int at = 0, last = worker < a.waves ? 1 : 0;
+    int empty = 0;                             // tiles before each group's own
     int64_t block_from = 0, block_to = 0;      // the block's tiles
     bool whole_block = false;                  // all of its waves have theirs
     if (balanced) {
@@ -105,13 +106,18 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
         uint32_t all;
         const int before = (int)block_excl_scan<kAttendThreads>((uint32_t)sum, s_red, &all);
         const int per = (int)attend_part(all, (uint32_t)a.waves);
+        empty = (int)attend_start(all, (uint32_t)a.waves, (uint32_t)per, (uint32_t)(a.n_tokens * hkv));
+        all += (uint32_t)(empty * a.n_tokens * hkv);
 #pragma unroll
         for (int i = 0; i < TPT; ++i) {
             const int t = tid * TPT + i;
-            s_ends[t] = before + ends[i];
-            if (blockIdx.x == 0 && t < a.n_tokens) a.ends[t] = before + ends[i];
+            s_ends[t] = before + ends[i] + (t + 1) * empty * hkv;
+            if (blockIdx.x == 0 && t < a.n_tokens) a.ends[t] = s_ends[t];
         }
-        if (blockIdx.x == 0 && tid == 0) a.ends[a.n_tokens] = per;
+        if (blockIdx.x == 0 && tid == 0) {
+            a.ends[a.n_tokens] = per;
+            a.ends[a.n_tokens + 1] = empty;
+        }
         __syncthreads();
         const int64_t from = (int64_t)worker * per;
         at = (int)min(from, (int64_t)all);
@@ -137,11 +143,11 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
             w.g = (at - start) / tiles;
             w.seq = __builtin_amdgcn_readfirstlane(s_seq[t]);
             w.span = span_of(a, w.seq, __builtin_amdgcn_readfirstlane(s_pos[t]));
-            w.lo = w.span.base + first * kAttendTile;
-            w.hi = min(w.span.len, w.lo + step * kAttendTile);
-            const int base = start + w.g * tiles;      // the group's first tile
-            w.joint = whole_block && block_from >= base && block_to <= base + tiles;
-            w.part = step == tiles ? -1 : (int64_t)(w.joint ? blockIdx.x * kAttendWaves : worker) + (int64_t)t * hkv + w.g;
+            w.lo = w.span.base + max(first - empty, 0) * kAttendTile;
+            w.hi = min(w.span.len, w.span.base + (first + step - empty) * kAttendTile);
+            const int end = start + (w.g + 1) * tiles, base = end - tiles + empty;     // the group's own tiles
+            w.joint = whole_block && block_from >= base && block_to <= end;
+            w.part = first <= empty && first + step == tiles ? -1 : (int64_t)(w.joint ? blockIdx.x * kAttendWaves : worker) + (int64_t)t * hkv + w.g;
         } else {
             const bool direct = a.split == ATTEND_DIRECT;
             const int chunk = worker % a.chunks, bg = worker / a.chunks;
@@ -636,9 +642,9 @@ __device__ __forceinline__ Half half_of(const PagesArgs &c, const int32_t *table
 // products are multiples of 2^-21 and sum exactly, kFlush tiles long, until the vector units
 // add them to acc; the low parts' sums, 2^-12 the size, may be biased.
 //
-// The vector units bound it, 60 % busy with the codes of both products and the weights' parts, and the
+// The vector units bound it, two thirds busy with the codes of both products and the weights' parts, and the
 // 7 us until the first tile is there: 131072 positions, 4 heads on each of 8, d = 128 take 33 us (4.6 TB/s);
-// without PACK, 32 ragged sequences of 7 heads on each of 4, 34 us (2.8 TB/s); with d = 64, 24.
+// without PACK, 32 ragged sequences of 7 heads on each of 4, 29 us (3.3 TB/s); with d = 64, 22.
 constexpr int kFlush = 4;
 template <typename T, int D, bool PACK>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend4(AttendArgs a)
@@ -979,9 +985,9 @@ __global__ __launch_bounds__(kMergeWaves * 64) void k_attend_merge(AttendArgs a)
     // parts `lead` .. lead + joints - 1 are blocks', every kAttendWaves-th number, the others waves'
     int lead = 0, joints = 0;
     if (a.split == ATTEND_BALANCED) {
-        const int per = a.ends[a.n_tokens], start = t > 0 ? a.ends[t - 1] : 0;
+        const int per = a.ends[a.n_tokens], empty = a.ends[a.n_tokens + 1], start = t > 0 ? a.ends[t - 1] : 0;
         const int tiles = (a.ends[t] - start) / a.c.n_kv_heads, from = start + g * tiles;
-        const AttendParts p = attend_parts(from, from + tiles, per);
+        const AttendParts p = attend_parts(from + empty, from + tiles, per);
         if (p.count == 1 && p.joints == 0) return;     // all in one wave, which wrote the output
         nch = p.count;
         lead = p.lead;

@@ -51,6 +51,7 @@ constexpr int kAttendDirect = 24;     // tiles
 constexpr int kAttendDirectF32 = 8;   // of f32 pages, whose tiles take three times as long
 constexpr int kAttendDirectFull = 64; // where there is a wave for every slot
 constexpr int kAttendPart = 2;        // fewest tiles of a BALANCED wave
+constexpr int kAttendStart = 2;       // tiles that the start of a BALANCED group counts as, at most
 constexpr int kAttendWaves = 4;       // of a block
 constexpr int kAttendTokens = 1024;
 constexpr int kAttendChunk = 512;     // rows
@@ -74,12 +75,12 @@ inline AttendPlan attend_plan(int64_t tokens, int64_t n_q_heads, int64_t n_kv_he
     const int64_t span = window > 0 && window + kAttendTile - 1 < max_len ? window + kAttendTile - 1 : max_len;
     const int64_t groups = tokens * n_kv_heads, tiles = ceil_div(span, kAttendTile);
     if (tiles <= (groups * kAttendWaves >= slots ? kAttendDirectFull : direct)) return p;
-    if (tokens <= kAttendTokens && groups * tiles < ((int64_t)1 << 31)) {
+    if (tokens <= kAttendTokens && groups * tiles < ((int64_t)1 << 30)) {
         p.split = ATTEND_BALANCED;
         const int64_t most = ceil_div(groups * tiles, kAttendPart);
         p.waves = most < slots ? most : slots;
         p.parts = p.waves + groups;
-        p.ends_bytes = ceil_div(4 * (tokens + 1), 64) * 64;
+        p.ends_bytes = ceil_div(4 * (tokens + 2), 64) * 64;
     } else {
         p.split = ATTEND_CHUNKED;
         p.chunks = ceil_div(span, kAttendChunk);
@@ -95,6 +96,15 @@ constexpr uint32_t attend_part(uint32_t all, uint32_t waves)
 {
     const uint32_t n = all / waves + (all % waves != 0);
     return n < (uint32_t)kAttendPart ? (uint32_t)kAttendPart : n;
+}
+
+// Empty tiles put before each group's, since a wave that comes to a new group begins again: as many
+// as fit what rounding up leaves of the waves' `per` tiles each, so that no wave takes longer for it.
+// 32 ragged sequences, 28 heads on 4, 4 bits: 38.1 us with none, 33.5 with one, 32.2 with two, 32.1 with four.
+constexpr uint32_t attend_start(uint32_t all, uint32_t waves, uint32_t per, uint32_t groups)
+{
+    const uint64_t n = ((uint64_t)per * waves - all) / groups;
+    return n < (uint64_t)kAttendStart ? (uint32_t)n : (uint32_t)kAttendStart;
 }
 
 // The parts of a group whose tiles are [from, to), `per` a wave: waves from `first` on, of which

@@ -371,3 +371,99 @@ def test_cache_formats_are_checked():
             R.PagedCache(k, k, table, par, par)
     with pytest.raises(R.RetopkError, match="bf16"):
         R.PagedCache.allocate("fp8", 2, 1, 16, 64, 1, 2, device="cpu")
+
+
+STARTS_PROGRAM = r"""
+#include "retopk_paged_plan.h"
+#include <cstdio>
+#include <vector>
+using namespace retopk;
+static int bad(const char *what, long long a, long long b) { printf("%s: %lld %lld\n", what, a, b); return 1; }
+int main()
+{
+    // BALANCED with empty tiles before each group's own: as the kernels walk them
+    uint32_t seed = 5;
+    int most_empty = 0;
+    auto rnd = [&](uint32_t n) { seed = seed * 1664525u + 1013904223u; return (seed >> 8) % n; };
+    for (int round = 0; round < 6000; ++round) {
+        const int tokens = 1 + rnd(round % 7 ? 12 : 1024), hkv = 1 + rnd(9), top = 1 + rnd(round % 3 ? 40 : 5000);
+        std::vector<int> tiles(tokens), ends(tokens);
+        int sum = 0, most = 0;
+        for (int t = 0; t < tokens; ++t) {
+            tiles[t] = round % 50 && rnd(4) ? (int)rnd(top + 1) : 0;
+            most = tiles[t] > most ? tiles[t] : most;
+            ends[t] = sum += tiles[t] * hkv;
+        }
+        const AttendPlan p = attend_plan(tokens, hkv, hkv, 64, (int64_t)(most <= kAttendDirectFull ? kAttendDirectFull + 1 : most) * kAttendTile, 0, 1 + rnd(2048), kAttendDirect);
+        if (p.split != ATTEND_BALANCED || p.ends_bytes < 4 * (tokens + 2)) return bad("split", tokens, p.split);
+        const int per = (int)attend_part(sum, (uint32_t)p.waves);
+        const int empty = (int)attend_start(sum, (uint32_t)p.waves, (uint32_t)per, (uint32_t)(tokens * hkv));
+        most_empty = empty > most_empty ? empty : most_empty;
+        const int all = sum + empty * tokens * hkv;
+        if (empty < 0 || (int64_t)per * p.waves < all) return bad("start", empty, all);
+        for (int t = 0; t < tokens; ++t) ends[t] += (t + 1) * empty * hkv;
+        std::vector<int> written(p.parts, -1);
+        std::vector<int> covered(tokens * hkv, 0), parts(tokens * hkv, 0), alone(tokens * hkv, 0);
+        for (int64_t b = 0; b < p.waves; ++b) {
+            const int64_t from = b * per, last = from + per < all ? from + per : all;
+            const int64_t block = b / kAttendWaves * kAttendWaves;
+            const bool whole = (block + kAttendWaves) * per <= all;
+            int shares = 0;
+            for (int64_t at = from; at < last;) {
+                int t = 0;
+                while (ends[t] <= at) ++t;
+                const int start = t ? ends[t - 1] : 0, n = (ends[t] - start) / hkv;
+                const int first = (int)(at - start) % n, g = (int)(at - start) / n, group = t * hkv + g;
+                const int step = n - first < last - at ? n - first : (int)(last - at);
+                const int lo = first > empty ? first - empty : 0, hi = first + step - empty;
+                const int end = start + (g + 1) * n, base = end - n + empty;
+                const bool joint = whole && block * per >= base && (block + kAttendWaves) * per <= end;
+                at += step;
+                if (joint && (shares || at < last || lo >= hi)) return bad("joint", b, group);
+                if (lo >= hi) continue;
+                ++shares;
+                if (covered[group] != lo) return bad("order", group, lo);
+                covered[group] = hi;
+                if (first <= empty && first + step == n) {
+                    alone[group] = 1;
+                    continue;
+                }
+                const int64_t id = (joint ? block : b) + group;
+                if (id >= p.parts || (written[id] >= 0 && !(joint && written[id] == group && b != block)))
+                    return bad("number", id, group);
+                if (!joint || b == block) parts[group] += 1;
+                written[id] = group;
+            }
+        }
+        for (int t = 0; t < tokens; ++t)
+            for (int g = 0; g < hkv; ++g) {
+                const int group = t * hkv + g, start = t ? ends[t - 1] : 0, n = (ends[t] - start) / hkv;
+                if (covered[group] != tiles[t]) return bad("covered", group, covered[group]);
+                const AttendParts q = attend_parts(start + g * n + empty, start + (g + 1) * n, per);
+                if (q.count == 1 && q.joints == 0) {
+                    if (parts[group] || !alone[group]) return bad("direct", group, parts[group]);
+                    continue;
+                }
+                if (alone[group] || q.count != parts[group]) return bad("count", q.count, parts[group]);
+                for (int c = 0; c < q.count; ++c) {
+                    const int extra = c < q.lead ? 0 : c < q.lead + q.joints ? c - q.lead : q.joints;
+                    const int64_t id = q.first + group + c + extra * (kAttendWaves - 1);
+                    if (id >= p.parts || written[id] != group) return bad("join", id, group);
+                    written[id] = -2;
+                }
+            }
+    }
+    if (most_empty != kAttendStart) return bad("never", most_empty, kAttendStart);
+    printf("ok\n");
+    return 0;
+}
+"""
+
+
+def test_plan_with_starts(tmp_path):
+    src, exe = tmp_path / "starts.cc", tmp_path / "starts"
+    src.write_text(STARTS_PROGRAM)
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Werror", "-I", B.CSRC, str(src), "-o",
+                    str(exe)], check=True)
+    res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and res.stdout.strip() == "ok", res.stdout
