@@ -92,33 +92,50 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
     int empty = 0;                             // tiles before each group's own
     int64_t block_from = 0, block_to = 0;      // the block's tiles
     bool whole_block = false;                  // all of its waves have theirs
+    // every token's last tile (of all KV heads), sequence and position, counted by each block for
+    // itself, or for up to 64 tokens by each wave, which then has no barrier to wait at
+    const bool few = a.n_tokens <= 64;
+    const int of = few ? tid & ~63 : 0;
+    int *const t_ends = s_ends + of, *const t_seq = s_seq + of, *const t_pos = s_pos + of;
     if (balanced) {
-        // every token's last tile (of all KV heads), counted by each block for itself
         int sum = 0, ends[TPT];
+        const int own = few ? 1 : TPT, t0 = few ? lane : tid * TPT;    // tokens of this thread
 #pragma unroll
         for (int i = 0; i < TPT; ++i) {
-            const int t = tid * TPT + i;
+            ends[i] = sum;
+            if (i >= own) continue;
+            const int t = t0 + i;
             const int sq = t < a.n_tokens ? a.seq[t] : -1, p = t < a.n_tokens ? a.pos[t] : -1;
-            s_seq[t] = sq;
-            s_pos[t] = p;
+            t_seq[t] = sq;
+            t_pos[t] = p;
             ends[i] = sum += span_of(a, sq, p).tiles() * hkv;
         }
         uint32_t all;
-        const int before = (int)block_excl_scan<kAttendThreads>((uint32_t)sum, s_red, &all);
+        int before;
+        if (few) {
+            const uint32_t incl = wave_incl_scan((uint32_t)sum);
+            all = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+            before = (int)incl - sum;
+        } else {
+            before = (int)block_excl_scan<kAttendThreads>((uint32_t)sum, s_red, &all);
+        }
         const int per = (int)attend_part(all, (uint32_t)a.waves);
         empty = (int)attend_start(all, (uint32_t)a.waves, (uint32_t)per, (uint32_t)(a.n_tokens * hkv));
         all += (uint32_t)(empty * a.n_tokens * hkv);
+        const bool tell = few ? worker == 0 : blockIdx.x == 0;         // the joining kernel
 #pragma unroll
         for (int i = 0; i < TPT; ++i) {
-            const int t = tid * TPT + i;
-            s_ends[t] = before + ends[i] + (t + 1) * empty * hkv;
-            if (blockIdx.x == 0 && t < a.n_tokens) a.ends[t] = s_ends[t];
+            if (i >= own) continue;
+            const int t = t0 + i;
+            t_ends[t] = before + ends[i] + (t + 1) * empty * hkv;
+            if (tell && t < a.n_tokens) a.ends[t] = t_ends[t];
         }
-        if (blockIdx.x == 0 && tid == 0) {
+        if (tell && tid == 0) {
             a.ends[a.n_tokens] = per;
             a.ends[a.n_tokens + 1] = empty;
         }
-        __syncthreads();
+        if (few) wave_lds_fence();
+        else __syncthreads();
         const int64_t from = (int64_t)worker * per;
         at = (int)min(from, (int64_t)all);
         last = (int)min(from + per, (int64_t)all);
@@ -133,16 +150,16 @@ __device__ __forceinline__ void for_shares(const AttendArgs &a, F f)
             // the token that holds tile `at`: as many as end at or before it come first
             int t = 0;
             for (int i = 0; i < a.n_tokens; i += 64)
-                t += __popcll(__ballot(i + lane < a.n_tokens && s_ends[i + lane] <= at));
+                t += __popcll(__ballot(i + lane < a.n_tokens && t_ends[i + lane] <= at));
             t = __builtin_amdgcn_readfirstlane(t);
-            const int start = t > 0 ? __builtin_amdgcn_readfirstlane(s_ends[t - 1]) : 0;
-            const int tiles = (__builtin_amdgcn_readfirstlane(s_ends[t]) - start) / hkv;
+            const int start = t > 0 ? __builtin_amdgcn_readfirstlane(t_ends[t - 1]) : 0;
+            const int tiles = (__builtin_amdgcn_readfirstlane(t_ends[t]) - start) / hkv;
             const int first = (at - start) % tiles;
             step = min(tiles - first, last - at);
             w.t = t;
             w.g = (at - start) / tiles;
-            w.seq = __builtin_amdgcn_readfirstlane(s_seq[t]);
-            w.span = span_of(a, w.seq, __builtin_amdgcn_readfirstlane(s_pos[t]));
+            w.seq = __builtin_amdgcn_readfirstlane(t_seq[t]);
+            w.span = span_of(a, w.seq, __builtin_amdgcn_readfirstlane(t_pos[t]));
             w.lo = w.span.base + max(first - empty, 0) * kAttendTile;
             w.hi = min(w.span.len, w.span.base + (first + step - empty) * kAttendTile);
             const int end = start + (w.g + 1) * tiles, base = end - tiles + empty;     // the group's own tiles

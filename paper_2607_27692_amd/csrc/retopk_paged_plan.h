@@ -103,8 +103,10 @@ constexpr uint32_t attend_part(uint32_t all, uint32_t waves)
 // 32 ragged sequences, 28 heads on 4, 4 bits: 38.1 us with none, 33.5 with one, 32.2 with two, 32.1 with four.
 constexpr uint32_t attend_start(uint32_t all, uint32_t waves, uint32_t per, uint32_t groups)
 {
-    const uint64_t n = ((uint64_t)per * waves - all) / groups;
-    return n < (uint64_t)kAttendStart ? (uint32_t)n : (uint32_t)kAttendStart;
+    const uint64_t left = (uint64_t)per * waves - all;
+    uint32_t n = 0;
+    while (n < (uint32_t)kAttendStart && (uint64_t)groups * (n + 1) <= left) ++n;
+    return n;
 }
 
 // The parts of a group whose tiles are [from, to), `per` a wave: waves from `first` on, of which
