@@ -34,9 +34,10 @@ constexpr uint32_t divide(uint32_t x, Divisor d)
 // three splits:
 //   DIRECT    one block a group: no group has more than a few tiles (kAttendDirect; twice and more
 //             where the groups alone fill the chip), and the block's waves join their results
-//             and write the output themselves.  One launch: 500 positions of 4 groups take 9.7 us
-//             from 4-bit pages and 12.7 in BALANCED's two, 1000 take 14.3 and 12.8; 2000 of
-//             1024 groups 43 and 52.
+//             and write the output themselves.  One launch: 512 positions of 8 KV heads take 9.0 us
+//             from 4-bit pages and 10.5 in BALANCED's two, 768 take 11.0 and 10.5, 1024 12.7 and
+//             10.5; of f32 pages 256 take 8.1 and 10.9, 384 11.2 and 11.6 (four query heads on each:
+//             17.7 and 15.2); 2000 of 1024 groups 43 and 52 from 4-bit pages.
 //   BALANCED  the tiles of all groups in one row, token after token, cut into equal parts on
 //             the device, one a wave, so that ragged lengths leave no wave idle; a part may
 //             span several groups and a group several parts.  At most kAttendTokens tokens,
@@ -47,10 +48,10 @@ constexpr uint32_t divide(uint32_t x, Divisor d)
 // part of a wave begins a new group, each part of a group a new wave).  Where all waves of a
 // block work on one group they join their results under the number of the first.
 constexpr int kAttendTile = 32;       // positions of a tile
-constexpr int kAttendDirect = 24;     // tiles
+constexpr int kAttendDirect = 20;     // tiles
 constexpr int kAttendDirectF32 = 8;   // of f32 pages, whose tiles take three times as long
 constexpr int kAttendDirectFull = 64; // where there is a wave for every slot
-constexpr int kAttendPart = 2;        // fewest tiles of a BALANCED wave
+constexpr int kAttendSimds = 1024;    // up to as many tiles a BALANCED wave takes one, of more two at least
 constexpr int kAttendStart = 2;       // tiles that the start of a BALANCED group counts as, at most
 constexpr int kAttendWaves = 4;       // of a block
 constexpr int kAttendTokens = 1024;
@@ -77,7 +78,8 @@ inline AttendPlan attend_plan(int64_t tokens, int64_t n_q_heads, int64_t n_kv_he
     if (tiles <= (groups * kAttendWaves >= slots ? kAttendDirectFull : direct)) return p;
     if (tokens <= kAttendTokens && groups * tiles < ((int64_t)1 << 30)) {
         p.split = ATTEND_BALANCED;
-        const int64_t most = ceil_div(groups * tiles, kAttendPart);
+        const int64_t all = groups * tiles, pairs = ceil_div(all, 2);
+        const int64_t most = all < kAttendSimds ? all : pairs > kAttendSimds ? pairs : kAttendSimds;
         p.waves = most < slots ? most : slots;
         p.parts = p.waves + groups;
         p.ends_bytes = ceil_div(4 * (tokens + 2), 64) * 64;
@@ -91,11 +93,12 @@ inline AttendPlan attend_plan(int64_t tokens, int64_t n_q_heads, int64_t n_kv_he
     return p;
 }
 
-// Tiles a BALANCED wave takes of `all`.
+// Tiles a BALANCED wave takes of `all`.  4096 positions of 8 heads, 1024 tiles, take 19.4 us from f32
+// pages with one each and 22.4 with two; 8192 take 27.0 and 24.2 (4 bits: 12.3 and 12.8, 13.9 and 12.9).
 constexpr uint32_t attend_part(uint32_t all, uint32_t waves)
 {
-    const uint32_t n = all / waves + (all % waves != 0);
-    return n < (uint32_t)kAttendPart ? (uint32_t)kAttendPart : n;
+    const uint32_t n = all / waves + (all % waves != 0), least = all > (uint32_t)kAttendSimds ? 2u : 1u;
+    return n < least ? least : n;
 }
 
 // Empty tiles put before each group's, since a wave that comes to a new group begins again: as many
