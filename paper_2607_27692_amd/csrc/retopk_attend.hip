@@ -9,9 +9,9 @@
 //   k_attend16  bf16:   both products on the matrix cores, weights in three bf16 parts
 //   k_attend    f32:    vector units
 // Measured, whole calls, the join's launch of about 5 us in them: 131072 positions, 32 heads on 8,
-// d = 128: 37 to 39 us from 4-bit pages (151 MB, 3.9 TB/s), 93 from bf16 pages (537 MB, 5.8 TB/s), 194
+// d = 128: 35 to 36 us from 4-bit pages (151 MB, 4.2 TB/s), 90 from bf16 pages (537 MB, 5.9 TB/s), 194
 // from f32 pages (1.07 GB, 5.5 TB/s); 32 ragged sequences of up to 16K positions, 28 heads on 4, 4 bits:
-// 32 us (96 MB, 3.0 TB/s).
+// 31 us (96 MB, 3.1 TB/s).
 #include "retopk.h"
 #include "retopk_paged.h"
 
@@ -411,7 +411,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void k_attend(AttendArgs a)
 // A weight is the sum of three bf16 parts (24 bits): column c has part c / GP of head c % GP, for
 // GP = 8 the third in a second product.  Products start from zero and are added by the vector units:
 // accumulated in the matrix cores the sums lose 2^-24 of the largest product at every step.  Bound by
-// HBM: the same positions take 88 us, 6.1 TB/s; 8 sequences of up to 32768 take 68 and the join.
+// HBM: the same positions take 85 to 88 us, 6.1 TB/s and more; 8 sequences of up to 32768 take 66 to 68.
 template <int D, int GP>
 __global__ __launch_bounds__(kAttendThreads, 2) void k_attend16(AttendArgs a)
 {
@@ -660,7 +660,7 @@ __device__ __forceinline__ Half half_of(const PagesArgs &c, const int32_t *table
 // add them to acc; the low parts' sums, 2^-12 the size, may be biased.
 //
 // The vector units bound it, two thirds busy with the codes of both products and the weights' parts, and the
-// 7 us until the first tile is there: 131072 positions, 4 heads on each of 8, d = 128 take 33 us (4.6 TB/s);
+// 6 us until the first tile is there: 131072 positions, 4 heads on each of 8, d = 128 take 33 us (4.6 TB/s);
 // without PACK, 32 ragged sequences of 7 heads on each of 4, 29 us (3.3 TB/s); with d = 64, 22.
 constexpr int kFlush = 4;
 template <typename T, int D, bool PACK>
