@@ -139,22 +139,32 @@ __device__ __forceinline__ void angle(double x, double &s, double &c)
 }
 
 // Cosines and sines of a block's tokens, a few angles a thread: pos * freq in float64, which
-// keeps every bit that float32 results show at any position.
-template <int D>
-__device__ __forceinline__ void block_angles(const retopk_rope &r, const int32_t *pos, int64_t t0, int64_t n,
-                                             bool inverse, double2 *s_cs)
-{
-    constexpr int TT = kRowThreads * 8 / D;
-    const int half = r.rot_dim / 2;
-    for (int i = threadIdx.x; i < TT * (D / 2); i += kRowThreads) {
-        const int tok = i / (D / 2), pair = i % (D / 2);
-        if (pair < half && t0 + tok < n) {
-            double s, c;
-            angle((double)pos[t0 + tok] * r.freq[pair], s, c);
-            s_cs[i] = make_double2(c * r.factor, (inverse ? -s : s) * r.factor);
+// keeps every bit that float32 results show at any position.  The positions are read apart, before
+// the first rows: loads return in order, and the angles would wait for the rows.
+template <int D> struct Angles {
+    static constexpr int TT = kRowThreads * 8 / D, N = TT * (D / 2) / kRowThreads;
+    int32_t p[N];
+
+    static __device__ __forceinline__ int token(int k) { return (threadIdx.x + k * kRowThreads) / (D / 2); }
+    __device__ __forceinline__ void read(const int32_t *pos, int64_t t0, int64_t n)
+    {
+#pragma unroll
+        for (int k = 0; k < N; ++k) p[k] = pos[min(t0 + token(k), n - 1)];
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __device__ __forceinline__ void make(const retopk_rope &r, bool inverse, double2 *s_cs) const
+    {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int i = threadIdx.x + k * kRowThreads, pair = i % (D / 2);
+            if (pair < r.rot_dim / 2) {
+                double s, c;
+                angle((double)p[k] * r.freq[pair], s, c);
+                s_cs[i] = make_double2(c * r.factor, (inverse ? -s : s) * r.factor);
+            }
         }
     }
-}
+};
 
 // A lane's elements e0 .. e0 + 7 of rows of one token: element i becomes
 // x[i] * c[i] + partner * s[i], the partner being the other element of its pair.
@@ -163,7 +173,7 @@ template <typename T, int D> struct Turn {
     int e0, half, rot, other;  // other: where the partners of a whole lane begin
     bool inside, lanes;        // partners in the lane itself; or all in one other lane
 
-    __device__ __forceinline__ void init(const retopk_rope &r, const double2 *cs, int lane_e0)
+    __device__ __forceinline__ void place(const retopk_rope &r, int lane_e0)
     {
         e0 = lane_e0;
         rot = r.rot_dim;
@@ -171,6 +181,9 @@ template <typename T, int D> struct Turn {
         inside = r.interleaved != 0;
         lanes = !inside && half % 8 == 0;
         other = e0 < half ? e0 + half : e0 < rot ? e0 - half : e0;
+    }
+    __device__ __forceinline__ void angles(const double2 *cs)
+    {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int e = e0 + i;
@@ -208,43 +221,59 @@ template <typename T, int D> struct Turn {
     }
 };
 
-// Walks a token's rows first .. last - 1, from `start` on and round to it, kAhead of them loaded
-// ahead of their use: at(h) is row h, and f(h, x) takes its elements, turned if h < n_rot.  In place:
-// a row's lanes are in one wave, and its loads, partners included, have all returned before
-// its stores.
+// Walks a token's rows first .. last - 1, from `begin` on and round to it, kAhead of them loaded
+// ahead of their use, the first ones by start(), before the angles are there: at(h) is row h, and f(h, x)
+// takes its elements, turned if h < n_rot.  In place: a row's lanes are in one wave, and its loads,
+// partners included, have all returned before its stores.
 constexpr int kAhead = 2;
-template <typename T, int D, typename At, typename F>
-__device__ __forceinline__ void walk_rows(const Turn<T, D> &turn, int e0, int first, int last, int start, int n_rot, At at, F f)
-{
+template <typename T, int D, typename At> struct Walk {
+    Turn<T, D> turn;
+    int e0, first, last, begin, n_rot;
+    At at;
     Oct<T> own[kAhead], partner[kAhead];
-    const int count = last - first;
-    auto nth = [&](int i) {
-        const int h = start + min(i, count - 1);
+
+    __device__ __forceinline__ int nth(int i) const
+    {
+        const int count = last - first, h = begin + min(i, count - 1);
         return h < last ? h : h - count;
-    };
-    auto load = [&](int i, Oct<T> &a, Oct<T> &b) {
+    }
+    __device__ __forceinline__ void load(int i, int u)
+    {
         const int h = nth(i);
         const T *row = at(h);
-        a.load(row + e0);
-        if (h < n_rot && turn.lanes) b.load(row + turn.other);
-    };
+        own[u].load(row + e0);
+        if (h < n_rot && turn.lanes) partner[u].load(row + turn.other);
+    }
+    __device__ __forceinline__ void start(const retopk_rope &r)
+    {
+        turn.place(r, e0);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) load(u, own[u], partner[u]);
-    for (int i0 = 0; i0 < count; i0 += kAhead) {
+        for (int u = 0; u < kAhead; ++u) load(u, u);
+    }
+    template <typename F> __device__ __forceinline__ void run(F f)
+    {
+        const int count = last - first;
+        for (int i0 = 0; i0 < count; i0 += kAhead) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int h = nth(i0 + u);
-            if (i0 + u < count) {
-                float x[8];
-                own[u].get(x);
-                if (h < n_rot) turn.turn(at(h), partner[u], x);
-                __builtin_amdgcn_sched_barrier(0);
-                load(i0 + u + kAhead, own[u], partner[u]);
-                __builtin_amdgcn_sched_barrier(0);
-                f(h, x);
+            for (int u = 0; u < kAhead; ++u) {
+                const int h = nth(i0 + u);
+                if (i0 + u < count) {
+                    float x[8];
+                    own[u].get(x);
+                    if (h < n_rot) turn.turn(at(h), partner[u], x);
+                    __builtin_amdgcn_sched_barrier(0);
+                    load(i0 + u + kAhead, u);
+                    __builtin_amdgcn_sched_barrier(0);
+                    f(h, x);
+                }
             }
         }
     }
+};
+template <typename T, int D, typename At>
+__device__ __forceinline__ Walk<T, D, At> walk_of(int e0, int first, int last, int begin, int n_rot, At at)
+{
+    return Walk<T, D, At>{{}, e0, first, last, begin, n_rot, at, {}, {}};
 }
 
 // rotary_embed.  Block (x, y): tokens x * TT .., heads y * per_block ..
@@ -255,16 +284,18 @@ __global__ __launch_bounds__(kRowThreads) void k_rotary(retopk_rope r, Rows<T> x
     constexpr int LPR = D / 8, TT = kRowThreads / LPR;
     __shared__ double2 s_cs[TT][D / 2];
     const int64_t t0 = (int64_t)blockIdx.x * TT;
-    block_angles<D>(r, pos, t0, n, inverse != 0, &s_cs[0][0]);
-    __syncthreads();
     const int tok = threadIdx.x / LPR, e0 = threadIdx.x % LPR * 8;
-    const int64_t t = t0 + tok;
-    if (t >= n) return;
-    Turn<T, D> turn;
-    turn.init(r, s_cs[tok], e0);
+    const int64_t t = min(t0 + tok, n - 1);            // lanes past the last token only read
     const int h0 = blockIdx.y * per_block, h1 = min(heads, h0 + per_block);
-    walk_rows(turn, e0, h0, h1, h0, heads, [&](int h) { return (const T *)x.at(t, h); },
-              [&](int h, const float (&v)[8]) { Oct<T>::store(out.at(t, h) + e0, v); });
+    auto walk = walk_of<T, D>(e0, h0, h1, h0, heads, [&](int h) { return (const T *)x.at(t, h); });
+    Angles<D> angles;
+    angles.read(pos, t0, n);
+    walk.start(r);
+    angles.make(r, inverse != 0, &s_cs[0][0]);
+    __syncthreads();
+    if (t0 + tok >= n) return;
+    walk.turn.angles(s_cs[tok]);
+    walk.run([&](int h, const float (&v)[8]) { Oct<T>::store(out.at(t, h) + e0, v); });
 }
 
 // ---------------------------------------------------------------------------
@@ -344,33 +375,31 @@ __global__ __launch_bounds__(kRowThreads) void k_append(PagesArgs c, retopk_rope
     const int64_t t0 = (int64_t)blockIdx.x * TT;
     const int heads = n_q + 2 * c.n_kv_heads, h0 = blockIdx.y * per_block;
     const int h1 = min(heads, h0 + per_block), n_rot = rotate ? n_q + c.n_kv_heads : 0;
-    if (h0 < n_rot) block_angles<D>(r, pos, t0, n, false, &s_cs[0][0]);
-    __syncthreads();
     const int tok = threadIdx.x / LPR, e0 = threadIdx.x % LPR * 8;
-    const int64_t t = t0 + tok;
-    if (t >= n) return;
-    const int32_t s = seq[t];
-    if (s < 0 || s >= c.n_seqs) return;
-    const int32_t row0 = row_of(c, s, pos[t], 0);
-    Turn<T, D> turn;
-    if (h0 < n_rot) turn.init(r, s_cs[tok], e0);
+    const int64_t t = min(t0 + tok, n - 1);            // lanes past the last token only read
     // blocks begin a quarter of their heads apart, so that some write queries while others are
     // busy with codes
-    const int start = h0 + (int)(blockIdx.x & 3) * (h1 - h0) / 4;
-    walk_rows(turn, e0, h0, h1, start, n_rot,
-              [&](int h) {
-                  return (const T *)(h < n_q ? q.at(t, h) : h < n_q + c.n_kv_heads ? k.at(t, h - n_q)
-                                                                                   : v.at(t, h - n_q - c.n_kv_heads));
-              },
-              [&](int h, const float (&x)[8]) {
-                  if (h < n_q) {
-                      Oct<T>::store(q_out.at(t, h) + e0, x);
-                  } else {
-                      const bool key = h < n_q + c.n_kv_heads;
-                      const int g = h - n_q - (key ? 0 : c.n_kv_heads);
-                      store_row<FMT, D, STREAM>(c, key, row0 < 0 ? -1 : row0 + g * c.page_size, e0, x);
-                  }
-              });
+    auto walk = walk_of<T, D>(e0, h0, h1, h0 + (int)(blockIdx.x & 3) * (h1 - h0) / 4, n_rot, [&](int h) {
+        return (const T *)(h < n_q ? q.at(t, h) : h < n_q + c.n_kv_heads ? k.at(t, h - n_q) : v.at(t, h - n_q - c.n_kv_heads));
+    });
+    const int32_t s = seq[t], p = pos[t];
+    Angles<D> angles;
+    if (h0 < n_rot) angles.read(pos, t0, n);
+    walk.start(r);
+    if (h0 < n_rot) angles.make(r, false, &s_cs[0][0]);
+    const int32_t row0 = row_of(c, s, p, 0);
+    __syncthreads();
+    if (t0 + tok >= n || s < 0 || s >= c.n_seqs) return;
+    if (h0 < n_rot) walk.turn.angles(s_cs[tok]);
+    walk.run([&](int h, const float (&x)[8]) {
+        if (h < n_q) {
+            Oct<T>::store(q_out.at(t, h) + e0, x);
+        } else {
+            const bool key = h < n_q + c.n_kv_heads;
+            const int g = h - n_q - (key ? 0 : c.n_kv_heads);
+            store_row<FMT, D, STREAM>(c, key, row0 < 0 ? -1 : row0 + g * c.page_size, e0, x);
+        }
+    });
 }
 
 // paged_gather.
