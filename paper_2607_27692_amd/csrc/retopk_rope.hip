@@ -7,8 +7,8 @@
 // tokens' cosines and sines in registers.  Consecutive tokens of one head lie side by side
 // in a page, so a block's writes of 4-bit rows are whole lines.  Bound by HBM, where a copy reaches
 // 4.7 TB/s: 8K tokens of 40 heads of 128 rotate in 39 us (168 MB, 4.3 TB/s); 16K tokens of 32 query and
-// 8 KV heads go to 4-bit pages in 91 (355 MB, 3.9); 64K rows of 8 heads are read back in 54 (344 MB,
-// most of it written, 6.4).  One token takes 4.0, 5.8 and 2.8 us.
+// 8 KV heads go to 4-bit pages in 87 (355 MB, 4.1); 64K rows of 8 heads are read back in 53 (344 MB,
+// most of it written, 6.5).  One token takes 4.1, 5.9 and 3.0 us.
 #include "retopk.h"
 #include "retopk_paged.h"
 
@@ -73,8 +73,10 @@ bool rows_ok(const retopk_rows &x, int64_t tokens, int64_t heads, int d, int es,
 namespace {
 
 constexpr int kRowThreads = 256;
-// Blocks that keep the chip's memory busy; a block walks over as many heads as that leaves.
-constexpr int64_t kRowBlocks = 1024;
+// Blocks that run at once on 256 CUs, four on each by the registers, five of those that put bf16 rows
+// into bf16 pages.  A few more than that cost a second round: 4099 tokens of 16 heads of 64, f32, rotate in
+// 9.7 us in 774 blocks and in 10.9 in 1032; 5 prompts in bf16 are appended in 21.4 us in 1280, in 22.5 in 960.
+constexpr int64_t kRowBlocks = 1024, kRowBlocksBf16 = 1280;
 constexpr int64_t kMaxGrid = ((int64_t)1 << 31) - 1;
 
 bool rope_ok(const retopk_rope *r, int d)
@@ -437,18 +439,19 @@ __global__ __launch_bounds__(kRowThreads) void k_gather(PagesArgs c, Rows<T> k, 
     }
 }
 
-// Grid of `heads` heads of n tokens, TT tokens to a block: the heads are shared out over
-// grid.y until there are kRowBlocks blocks, or one a head.
+// Grid of `heads` heads of n tokens, TT tokens to a block: the heads are shared out evenly over
+// grid.y, as far as all blocks run at once, or to one a head.
 struct RowGrid {
     dim3 grid;
     int per_block;
 };
-bool row_grid(int64_t n, int d, int64_t heads, RowGrid *out)
+bool row_grid(int64_t n, int d, int64_t heads, int64_t blocks, RowGrid *out)
 {
     const int64_t tiles = ceil_div(n, kRowThreads * 8 / d);
     if (tiles > kMaxGrid || heads > 65535) return false;
-    int64_t per = heads * tiles / kRowBlocks;
-    per = per < 1 ? 1 : per > heads ? heads : per;
+    int64_t shares = blocks / tiles;
+    shares = shares < 1 ? 1 : shares > heads ? heads : shares;
+    const int64_t per = ceil_div(heads, shares);
     out->per_block = (int)per;
     out->grid = dim3((unsigned)tiles, (unsigned)ceil_div(heads, per));
     return true;
@@ -574,7 +577,7 @@ retopk_status rotary_embed(const retopk_rope *r, int32_t dtype, int32_t head_dim
     if (x.p == out.p && (x.token_stride != out.token_stride || x.head_stride != out.head_stride))
         return RETOPK_ERR_ARG;
     RowGrid g;
-    if (!row_grid(n_tokens, head_dim, n_heads, &g)) return RETOPK_ERR_UNSUPPORTED;
+    if (!row_grid(n_tokens, head_dim, n_heads, kRowBlocks, &g)) return RETOPK_ERR_UNSUPPORTED;
     by_type(dtype, head_dim, [&](auto zero, auto d) {
         using T = decltype(zero);
         hipLaunchKernelGGL((k_rotary<T, decltype(d)::value>), g.grid, dim3(kRowThreads), 0, (hipStream_t)stream, *r,
@@ -604,7 +607,9 @@ retopk_status paged_append(const retopk_pages *c, const retopk_rope *r, int32_t 
             return RETOPK_ERR_ARG;
     }
     RowGrid g;
-    if (!row_grid(n_tokens, d, (int64_t)n_q_heads + 2 * (int64_t)c->n_kv_heads, &g)) return RETOPK_ERR_UNSUPPORTED;
+    if (!row_grid(n_tokens, d, (int64_t)n_q_heads + 2 * (int64_t)c->n_kv_heads,
+                  c->format == RETOPK_PAGES_BF16 ? kRowBlocksBf16 : kRowBlocks, &g))
+        return RETOPK_ERR_UNSUPPORTED;
     const int64_t row = c->format == RETOPK_PAGES_Q4 ? d / 2 : d * es;
     const bool past = 2 * n_tokens * c->n_kv_heads * row > kStreamBytes;
     const PagesArgs a = pages_args(*c);
@@ -629,7 +634,7 @@ retopk_status paged_gather(const retopk_pages *c, int32_t dtype, int64_t n_token
         (v.p && !rows_ok(v, n_tokens, c->n_kv_heads, d, es, true)))
         return RETOPK_ERR_ARG;
     RowGrid g;
-    if (!row_grid(n_tokens, d, 2 * (int64_t)c->n_kv_heads, &g)) return RETOPK_ERR_UNSUPPORTED;
+    if (!row_grid(n_tokens, d, 2 * (int64_t)c->n_kv_heads, kRowBlocks, &g)) return RETOPK_ERR_UNSUPPORTED;
     const bool past = 2 * n_tokens * c->n_kv_heads * d * es > kStreamBytes;
     const PagesArgs a = pages_args(*c);
     by_type(dtype, d, [&](auto zero, auto dim) {
