@@ -7,8 +7,8 @@
 // tokens' cosines and sines in registers.  Consecutive tokens of one head lie side by side
 // in a page, so a block's writes of 4-bit rows are whole lines.  Bound by HBM, where a copy reaches
 // 4.7 TB/s: 8K tokens of 40 heads of 128 rotate in 39 us (168 MB, 4.3 TB/s); 16K tokens of 32 query and
-// 8 KV heads go to 4-bit pages in 87 (355 MB, 4.1); 64K rows of 8 heads are read back in 53 (344 MB,
-// most of it written, 6.5).  One token takes 4.1, 5.9 and 3.0 us.
+// 8 KV heads go to 4-bit pages in 84 (355 MB, 4.2); 64K rows of 8 heads are read back in 53 (344 MB,
+// most of it written, 6.5).  One token takes 4 to 5, 5.6 and 2.9 us.
 #include "retopk.h"
 #include "retopk_paged.h"
 
