@@ -478,6 +478,9 @@ def test_attention(fmt, dtype, d, hq, hkv, page, lens, window):
     ("f32", "f32", 128, 1, 1, 100, 520, 2048, 1000),
     # hundreds of tokens shared out tile by tile, most of them short
     ("q4", "f32", 128, 8, 1, 16, 700, 2600, 0), ("bf16", "bf16", 128, 8, 1, 64, 513, 2500, 0),
+    # as many as a wave counts by itself, and one more
+    ("q4", "bf16", 64, 4, 1, 16, 64, 1500, 0), ("f32", "f32", 64, 3, 1, 7, 64, 1500, 700),
+    ("bf16", "bf16", 64, 2, 1, 32, 65, 1500, 0), ("q4", "f32", 128, 8, 2, 32, 65, 2000, 0),
 ])
 def test_attention_of_many_tokens(fmt, dtype, d, hq, hkv, page, tokens, longest, window):
     """Queries of many tokens over a few sequences, at every kind of split; some of them checked."""
